@@ -364,6 +364,158 @@ int32_t aha_profile_events(void *const *events, int32_t count);
  */
 int32_t aha_exchange_looks(int32_t looks);
 
+/*
+ * ---- A prompt that several sequences continue -------------------------------
+ *
+ * The operations above evict the cache of one prompt.  The three below serve
+ * what comes before and after it: the rotation of queries and keys by their
+ * positions, a cache in pages that grows token by token, and the attention of
+ * the new tokens of a batch whose sequences share prefixes (a compact cache that
+ * aha_compact_kv has filled, or a prompt's own keys and values) and go on with
+ * tails of their own in the paged cache.  They keep the general rules above.
+ */
+
+enum { AHA_PAIR_HALVES = 0, AHA_PAIR_NEIGHBOURS = 1 };
+
+/*
+ * Rotation by positions.  Of a row's head_dim channels the first rot_dim are
+ * turned in rot_dim / 2 pairs, the others pass through.  Pair f of a row is
+ *
+ *   (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t),
+ *   t = positions[axis f][row] * inv_freq[f],
+ *
+ * its channels f and f + rot_dim / 2 (AHA_PAIR_HALVES) or 2 f and 2 f + 1
+ * (AHA_PAIR_NEIGHBOURS).  The angle is formed in double precision, so that far
+ * positions lose nothing, the products in fp32.
+ *
+ *  inv_freq   DEVICE fp32 [rot_dim / 2]: radians per position of every pair.
+ *  pair_axis  DEVICE int32 [rot_dim / 2] or NULL (axis 0 for all): which of the
+ *             n_axes positions turns a pair (values outside are clamped).
+ *  positions  DEVICE int32 dense [n_axes, batch, tokens]; any int32 value.
+ *  transpose  non-zero: every pair is turned by -t.  The rotation is orthogonal,
+ *             so this is its inverse and carries gradients of the outputs back to
+ *             the inputs.
+ */
+typedef struct aha_rotary {
+    int32_t batch;        /* batch * tokens <= 2^30 */
+    int32_t tokens;       /* rows per sequence and head */
+    int32_t n_q_heads;    /* any two numbers >= 1 */
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* 64 or 128 */
+    int32_t dtype;        /* AHA_F32 | AHA_BF16 */
+    int32_t rot_dim;      /* a multiple of 16, 0..head_dim */
+    int32_t pairing;      /* AHA_PAIR_HALVES | AHA_PAIR_NEIGHBOURS */
+    int32_t n_axes;       /* 1..4 */
+    int32_t transpose;    /* 0 | 1 */
+    int64_t q_stride[3];  /* elements: batch, head, token */
+    int64_t k_stride[3];
+    int64_t v_stride[3];  /* aha_append_paged */
+    int64_t q_out_stride[3];
+    int64_t k_out_stride[3]; /* aha_rotate */
+} aha_rotary;
+
+/*
+ * A cache in pages: token s of sequence b lies in row s % page_size of page
+ * page_table[b][s / page_size], the same page and row of both pools and for all
+ * KV heads.
+ *
+ *  page_table  DEVICE int32 dense [batch, table_width].  An entry outside
+ *              [0, n_pages) is a hole: nothing is written there and no row
+ *              attends to its tokens (a page that was given back).
+ */
+typedef struct aha_pages {
+    int32_t n_pages;      /* of the pools, <= 2^30 */
+    int32_t page_size;    /* tokens: a power of two, 1..1024 */
+    int32_t table_width;  /* table_width * page_size <= 2^30 */
+    int32_t reserved;     /* must be 0 */
+    int64_t k_stride[3];  /* elements: page, head, row */
+    int64_t v_stride[3];
+} aha_pages;
+
+/*
+ * Rotates queries and keys: q_out[b, h, t, :] and k_out[b, h, t, :] are the rows
+ * of q [batch, n_q_heads, tokens, head_dim] and k [batch, n_kv_heads, ...] turned.
+ * q (with q_out) or k (with k_out) may be null.  An output may be its input
+ * (same pointer and strides), which is then turned in place; otherwise they must
+ * not overlap.
+ */
+int32_t aha_rotate(const aha_rotary *p, const void *q, const void *k, const float *inv_freq,
+                   const int32_t *pair_axis, const int32_t *positions, void *q_out,
+                   void *k_out, void *stream);
+
+/*
+ * Appends the new tokens of a batch to the paged cache: row t < new_len[b] of
+ * sequence b becomes token tail_len[b] - new_len[b] + t of its tail: the row of
+ * k, turned as by aha_rotate, and the row of v as it is.  The rows of q are turned into q_out
+ * (both may be null).
+ *
+ *  tail_len  DEVICE int32 [batch]: tokens of each tail, the new ones counted.
+ *  new_len   DEVICE int32 [batch] or NULL (all `tokens` rows are real): clamped to
+ *            [0, tokens].  Rows from new_len[b] on are padding: nothing is read
+ *            for them, their rows of q_out stay as they are.
+ * A token before 0, behind the table's last page or in a hole is dropped.  No two
+ * tokens of a call may have the same place; the place then holds one of the two.
+ */
+int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void *q,
+                         const void *k, const void *v, const float *inv_freq,
+                         const int32_t *pair_axis, const int32_t *positions,
+                         const int32_t *page_table, const int32_t *tail_len,
+                         const int32_t *new_len, void *q_out, void *k_pages, void *v_pages,
+                         void *stream);
+
+/*
+ * Attention of a batch's new tokens behind shared prefixes.
+ *
+ *   out[b, h, t, :] = sum_j softmax_j(scale * q[b, h, t] . K_j) V_j,   t < new_len[b],
+ *
+ * over all prefix_len[g] tokens of the sequence's prefix g and the tokens
+ * 0 .. tail_len[b] - new_len[b] + t of its tail (its own and earlier new tokens among
+ * them, which aha_append_paged has written).  Sequences
+ * prefix_first[g] .. prefix_first[g + 1] - 1 share prefix g, whose keys and values are
+ * read once for all of them.
+ *
+ *  prefix_len    DEVICE int32 [n_prefixes], clamped to [0, prefix_cap].
+ *  prefix_first  DEVICE int32 [n_prefixes + 1], ascending, within [0, batch]; sequences
+ *                before the first and behind the last entry have no prefix.
+ *  k_prefix, v_prefix  [n_prefixes, n_kv_heads, prefix_cap, head_dim] by stride.
+ *  pages, k_pages, v_pages, page_table, tail_len  the tails; all null: no tails.
+ *  new_len       as for aha_append_paged; rows from new_len[b] on are neither read
+ *                nor written in out and lse.
+ *  lse           out, fp32 dense [batch, n_q_heads, q_len] or NULL: natural logarithm of
+ *                sum_j exp(scale * q . K_j).
+ * A row without a key gets zeros, and -inf in lse.  Keys and values that no row of the
+ * sequence sees are not looked at: they may hold anything.  (Within a chunk, q_len > 1, the VALUES of
+ * a sequence's new tokens have to be finite for its earlier ones.)
+ * The lengths and tables are read on the device, so that a captured call follows them.
+ */
+typedef struct aha_shared {
+    int32_t batch;        /* batch * n_kv_heads <= 65535 */
+    int32_t q_len;        /* rows per sequence, >= 1; n_q_heads / n_kv_heads * q_len * batch <= 2^24 */
+    int32_t n_q_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* 64 or 128 */
+    int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, prefixes, pools and out */
+    int32_t n_prefixes;   /* 0..65535; 0: the prefix arguments are not looked at */
+    int32_t prefix_cap;   /* <= 2^30 */
+    float scale;          /* >= 0, finite */
+    int32_t reserved;     /* must be 0 */
+    int64_t q_stride[3];  /* elements: batch, head, token */
+    int64_t out_stride[3];
+    int64_t k_stride[3];  /* elements: prefix, head, token */
+    int64_t v_stride[3];
+} aha_shared;
+
+/* `pages` may be null (no tails); of it only the sizes are looked at. */
+int32_t aha_shared_attention_workspace_bytes(const aha_shared *p, const aha_pages *pages,
+                                             size_t *out_bytes);
+int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const void *q,
+                             const void *k_prefix, const void *v_prefix,
+                             const int32_t *prefix_len, const int32_t *prefix_first,
+                             const void *k_pages, const void *v_pages,
+                             const int32_t *page_table, const int32_t *tail_len,
+                             const int32_t *new_len, void *out, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /* Thread-local description of the last error returned on this thread. */
 const char *aha_last_error(void);
 

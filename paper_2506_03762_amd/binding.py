@@ -26,6 +26,7 @@ AHA_ERR_WORKSPACE = -3
 AHA_ERR_HIP = -4
 AHA_F32, AHA_BF16 = 0, 1
 AHA_SCALE_FIXED, AHA_SCALE_ADAPTIVE = 0, 1
+AHA_PAIR_HALVES, AHA_PAIR_NEIGHBOURS = 0, 1
 
 # entry points returning an int32 status first, then the two that return strings
 EXPORTS = ("aha_workspace_bytes", "aha_prefill_scores", "aha_prefill_scores_lse",
@@ -33,7 +34,8 @@ EXPORTS = ("aha_workspace_bytes", "aha_prefill_scores", "aha_prefill_scores_lse"
            "aha_prefill_row_stats", "aha_window_attention_workspace_bytes",
            "aha_prefill_window_attention", "aha_select_topk",
            "aha_compact_kv", "aha_decode_step", "aha_decode_step_static", "aha_profile_events",
-           "aha_exchange_looks", "aha_last_error",
+           "aha_exchange_looks", "aha_rotate", "aha_append_paged",
+           "aha_shared_attention_workspace_bytes", "aha_shared_attention", "aha_last_error",
            "aha_version")
 
 
@@ -56,6 +58,25 @@ class aha_params(ctypes.Structure):
         ("score_pool", ctypes.c_int32), ("sink", ctypes.c_int32),
         ("decode_value_prior", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class aha_rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "tokens", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "rot_dim", "pairing", "n_axes",
+        "transpose")] + [(n, ctypes.c_int64 * 3) for n in (
+            "q_stride", "k_stride", "v_stride", "q_out_stride", "k_out_stride")]
+
+
+class aha_pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "table_width", "reserved")] + [
+        (n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride")]
+
+
+class aha_shared(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "q_len", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "n_prefixes", "prefix_cap")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64 * 3) for n in (
+            "q_stride", "out_stride", "k_stride", "v_stride")]
 
 
 _lib = None
@@ -86,6 +107,11 @@ def load() -> ctypes.CDLL:
     lib.aha_decode_step_static.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]
     lib.aha_profile_events.argtypes = [ctypes.POINTER(vp), i32]
     lib.aha_exchange_looks.argtypes = [i32]
+    rp, gp, sp = (ctypes.POINTER(t) for t in (aha_rotary, aha_pages, aha_shared))
+    lib.aha_rotate.argtypes = [rp] + [vp] * 8
+    lib.aha_append_paged.argtypes = [rp, gp] + [vp] * 13
+    lib.aha_shared_attention_workspace_bytes.argtypes = [sp, gp, ctypes.POINTER(sz)]
+    lib.aha_shared_attention.argtypes = [sp, gp] + [vp] * 13 + [sz, vp]
     for name in EXPORTS[:-2]:
         getattr(lib, name).restype = i32
     lib.aha_last_error.restype = ctypes.c_char_p
@@ -308,3 +334,173 @@ class CompactCache:
 
 def default_fixed_scale(head_dim: int) -> float:
     return 1.0 / math.sqrt(head_dim)
+
+
+# ---- a prompt that several sequences continue: rotation, the paged cache, attention behind shared prefixes ----
+# A description is made once (its C struct is built then, and the sizes that its tensors have) and serves every call
+# with tensors of these shapes and strides.  Per call their element types, sizes and devices are compared, not their
+# strides: 0.2 us a tensor.
+
+_CODES = {torch.float32: AHA_F32, torch.bfloat16: AHA_BF16}
+# what has no strides of its own
+_DENSE = ("inv_freq", "pair_axis", "positions", "page_table", "tail_len", "new_len", "prefix_len", "prefix_first", "lse")
+
+
+def _view(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """Strides (first three axes) of a [., heads, ., d] view whose channels are contiguous."""
+    if t.dim() != 4 or (t.stride(3) != 1 and t.size(3) > 1) or t.dtype not in _CODES:
+        raise ValueError("%s must be a 4-dimensional fp32 or bf16 view with contiguous channels" % name)
+    if like is not None and (t.dtype != like.dtype or t.size(3) != like.size(3)):
+        raise ValueError("%s has another dtype or head size" % name)
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+class _Described:
+    """The C struct of a description, its rows' (batch, KV heads, head size, dtype), and of its tensors, in the order
+    in which a call takes them, names, element types and numbers of elements."""
+
+    def __init__(self, struct, rows, *tensors):
+        self._as_parameter_ = ctypes.byref(struct)
+        self.struct, self.rows = struct, rows
+        self.tensors = tuple(t + (t[0] in _DENSE,) for t in tensors)
+
+
+def _check_tensors(tensors, given):
+    device = torch._C._cuda_getDevice()
+    for (name, dtype, n, dense), t in zip(tensors, given):
+        if t is not None and (t.dtype is not dtype or t.numel() != n or t.get_device() != device or
+                              (dense and not t.is_contiguous())):
+            raise ValueError("%s: not a%s tensor of %d elements of %s on the current device" % (
+                name, " contiguous" if dense else "", n, dtype))
+
+
+class Rotary(_Described):
+    """Description of a rotation (aha_rotary of include/aha.h)."""
+
+    @classmethod
+    def of(cls, q, k, q_out=None, k_out=None, v=None, *, rot_dim: Optional[int] = None, n_axes: int = 1,
+           pairing: int = AHA_PAIR_HALVES, transpose: int = 0) -> "Rotary":
+        """For q [b, Hq, n, d] and k [b, Hkv, n, d] views (either may be None), what they are turned into and,
+        to append, the values."""
+        given = k if k is not None else q
+        if given is None:
+            raise ValueError("q and k are both None")
+        p = aha_rotary(batch=given.size(0), tokens=given.size(2), head_dim=given.size(3), pairing=pairing,
+                       n_q_heads=1 if q is None else q.size(1), n_kv_heads=1 if k is None else k.size(1),
+                       dtype=_CODES.get(given.dtype, -1), n_axes=n_axes, transpose=transpose,
+                       rot_dim=given.size(3) if rot_dim is None else rot_dim)
+        for name, t in (("q", q), ("k", k), ("v", v), ("q_out", q_out), ("k_out", k_out)):
+            if t is not None:
+                setattr(p, name + "_stride", _view(name, t, given))
+        if q is not None and k is not None and (q.size(0), q.size(2)) != (k.size(0), k.size(2)):
+            raise ValueError("q and k have other batches or tokens")
+        rows, dt, pairs = p.batch * p.tokens * p.head_dim, given.dtype, p.rot_dim // 2
+        nq, nk = rows * p.n_q_heads, rows * p.n_kv_heads
+        self = cls(p, (p.batch, p.n_kv_heads, p.head_dim, dt), ("q", dt, nq), ("k", dt, nk),
+                   ("inv_freq", torch.float32, pairs), ("pair_axis", torch.int32, pairs),
+                   ("positions", torch.int32, p.n_axes * p.batch * p.tokens), ("q_out", dt, nq), ("k_out", dt, nk))
+        self.appended = self.tensors[:6] + (("v", dt, nk, False),)
+        return self
+
+
+class Pages(_Described):
+    """Description of a paged cache (aha_pages)."""
+
+    @classmethod
+    def of(cls, k_pages, v_pages, page_table) -> "Pages":
+        """For pools [pages, Hkv, page size, d] (views by stride) and a table [b, width]."""
+        p = aha_pages(n_pages=k_pages.size(0), page_size=k_pages.size(2), table_width=page_table.size(1),
+                      k_stride=_view("k_pages", k_pages), v_stride=_view("v_pages", v_pages, k_pages))
+        if k_pages.shape != v_pages.shape:
+            raise ValueError("the pools have different shapes")
+        n, batch = k_pages.numel(), page_table.size(0)
+        return cls(p, (batch, k_pages.size(1), k_pages.size(3), k_pages.dtype),
+                   ("k_pages", k_pages.dtype, n), ("v_pages", k_pages.dtype, n),
+                   ("page_table", torch.int32, page_table.numel()), ("tail_len", torch.int32, batch),
+                   ("new_len", torch.int32, batch))
+
+
+class SharedAttention(_Described):
+    """Description of an attention behind shared prefixes (aha_shared)."""
+
+    @classmethod
+    def of(cls, q, out, k_prefix=None, v_prefix=None, scale: Optional[float] = None, *, n_kv_heads: Optional[int] = None
+           ) -> "SharedAttention":
+        """For q and out [b, Hq, n, d] and the prefixes [prefixes, Hkv, capacity, d] (None: none; the number of KV
+        heads then has to be given).  scale None: 1 / sqrt(d)."""
+        if k_prefix is None and n_kv_heads is None:
+            raise ValueError("neither prefixes nor n_kv_heads are given")
+        p = aha_shared(batch=q.size(0), q_len=q.size(2), n_q_heads=q.size(1), head_dim=q.size(3),
+                       n_kv_heads=n_kv_heads if k_prefix is None else k_prefix.size(1),
+                       dtype=_CODES.get(q.dtype, -1), scale=default_fixed_scale(q.size(3)) if scale is None else scale,
+                       q_stride=_view("q", q), out_stride=_view("out", out, q))
+        if q.shape != out.shape or (k_prefix is not None and k_prefix.shape != v_prefix.shape):
+            raise ValueError("q and out, or the prefixes' keys and values, have different shapes")
+        n = 0
+        if k_prefix is not None:
+            n, p.n_prefixes, p.prefix_cap = k_prefix.numel(), k_prefix.size(0), k_prefix.size(2)
+            p.k_stride, p.v_stride = _view("k_prefix", k_prefix, q), _view("v_prefix", v_prefix, q)
+        return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), ("q", q.dtype, q.numel()),
+                   ("k_prefix", q.dtype, n), ("v_prefix", q.dtype, n), ("prefix_len", torch.int32, p.n_prefixes), ("prefix_first", torch.int32, p.n_prefixes + 1),
+                   ("out", q.dtype, q.numel()), ("lse", torch.float32, q.numel() // p.head_dim),
+                   ("new_len", torch.int32, p.batch))
+
+
+def rotary_tables(rot_dim: int, base: float = 10000.0, sections=None, device="cuda"):
+    """(inv_freq, pair_axis) of rot_dim / 2 pairs: base^(-2 f / rot_dim) radians per position, and the axis that
+    turns each pair: None, or runs of sections[a] pairs for axis a."""
+    if sections is not None and sum(sections) != rot_dim // 2:
+        raise ValueError("sections must add up to rot_dim / 2 pairs")
+    f = torch.arange(rot_dim // 2, dtype=torch.float64)
+    inv_freq = (base ** (-2.0 * f / max(1, rot_dim))).float().to(device)
+    if sections is None:
+        return inv_freq, None
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    return inv_freq, torch.tensor(axis, dtype=torch.int32, device=device)
+
+
+def aha_rotate(p: Rotary, q, k, inv_freq, pair_axis, positions, q_out, k_out):
+    """q_out, k_out <- the rows of q, k turned by positions [axes, b, n] (int32)."""
+    _check_tensors(p.tensors, (q, k, inv_freq, pair_axis, positions, q_out, k_out))
+    _check((_lib or load()).aha_rotate(
+        p, _ptr(q), _ptr(k), _ptr(inv_freq), _ptr(pair_axis), _ptr(positions), _ptr(q_out), _ptr(k_out), _stream()))
+
+
+def aha_append_paged(p: Rotary, cache: Pages, q, k, v, inv_freq, pair_axis, positions, page_table, tail_len, new_len,
+                     q_out, k_pages, v_pages):
+    """The new tokens' keys (turned) and values into their places of the pools; q_out <- q turned."""
+    _check_tensors(p.appended, (q, k, inv_freq, pair_axis, positions, q_out, v))
+    _check_tensors(cache.tensors, (k_pages, v_pages, page_table, tail_len, new_len))
+    _check_same(p, cache)
+    _check((_lib or load()).aha_append_paged(
+        p, cache, _ptr(q), _ptr(k), _ptr(v), _ptr(inv_freq), _ptr(pair_axis), _ptr(positions), _ptr(page_table),
+        _ptr(tail_len), _ptr(new_len), _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _stream()))
+
+
+def _check_same(p, cache: Pages):
+    """The rows' batch, KV heads, head size and element type are the cache's."""
+    if cache.rows != p.rows:
+        raise ValueError("the cache is one of %s (batch, KV heads, head size, dtype), the rows are of %s" % (cache.rows, p.rows))
+
+
+def shared_attention_workspace_bytes(p: SharedAttention, cache: Optional[Pages]) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().aha_shared_attention_workspace_bytes(p, cache, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_shared_workspace(p: SharedAttention, cache: Optional[Pages], device="cuda") -> torch.Tensor:
+    return torch.empty(max(shared_attention_workspace_bytes(p, cache), 256), dtype=torch.uint8, device=device)
+
+
+def aha_shared_attention(p: SharedAttention, cache: Optional[Pages], q, k_prefix, v_prefix, prefix_len, prefix_first,
+                         k_pages, v_pages, page_table, tail_len, new_len, out, lse, workspace):
+    """out [b, Hq, n, d], lse [b, Hq, n] (fp32 or None) <- attention of the new tokens over their shared prefix
+    and their own tail."""
+    _check_tensors(p.tensors, (q, k_prefix, v_prefix, prefix_len, prefix_first, out, lse, new_len))
+    if cache is not None:
+        _check_tensors(cache.tensors, (k_pages, v_pages, page_table, tail_len))
+        _check_same(p, cache)
+    _check((_lib or load()).aha_shared_attention(
+        p, cache, _ptr(q), _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_len), _ptr(prefix_first), _ptr(k_pages),
+        _ptr(v_pages), _ptr(page_table), _ptr(tail_len), _ptr(new_len), _ptr(out), _ptr(lse), *_ws(workspace), _stream()))

@@ -24,16 +24,13 @@ static hipError_t stage(int i, hipStream_t st) {
 // (fewer: patience).
 constexpr int32_t kLooks = 4000;
 
-static int32_t fail(int32_t code, const char *fmt, ...) {
+int32_t fail(int32_t code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof(g_err), fmt, ap);
     va_end(ap);
     return code;
 }
-
-static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-static inline int esize(int dtype) { return dtype == AHA_BF16 ? 2 : 4; }
 
 // Checks shared by all entry points.
 static int32_t check_common(const aha_params *p) {
@@ -68,7 +65,7 @@ static int32_t check_common(const aha_params *p) {
     return AHA_OK;
 }
 
-static int32_t check_stride(const char *name, const int64_t s[3], int dtype, int d) {
+int32_t check_stride(const char *name, const int64_t s[3], int dtype, int d) {
     const int a = 16 / esize(dtype);
     for (int t = 0; t < 3; ++t)
         if (s[t] < 0 || s[t] % a != 0)
@@ -120,7 +117,7 @@ static int32_t check_compact(const aha_params *p) {
     return check_stride("v", p->v_stride, p->dtype, p->head_dim);
 }
 
-static int32_t check_ptr(const char *name, const void *ptr, size_t align) {
+int32_t check_ptr(const char *name, const void *ptr, size_t align) {
     if (!ptr) return fail(AHA_ERR_INVALID_ARG, "%s is null", name);
     if ((uintptr_t)ptr % align != 0)
         return fail(AHA_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
@@ -630,7 +627,7 @@ static DecodePlan plan_decode(const aha_params *p, size_t limit = SIZE_MAX) {
     return pl;
 }
 
-static int32_t check_ws(const void *ws, size_t have, size_t need) {
+int32_t check_ws(const void *ws, size_t have, size_t need) {
     if (need == 0) return AHA_OK;
     if (!ws) return fail(AHA_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", need);
     if ((uintptr_t)ws % 256 != 0) return fail(AHA_ERR_WORKSPACE, "workspace is not 256-byte aligned");
@@ -639,7 +636,7 @@ static int32_t check_ws(const void *ws, size_t have, size_t need) {
     return AHA_OK;
 }
 
-static int32_t hip_result(hipError_t e, const char *what) {
+int32_t hip_result(hipError_t e, const char *what) {
     if (e == hipSuccess) return AHA_OK;
     return fail(AHA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }

@@ -29,6 +29,15 @@ inline hipError_t device_once(DeviceOnce &o, F fn) {
     return o.err[dev];
 }
 
+// What the entry points check and report with (aha_api.hip).
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline int esize(int dtype) { return dtype == AHA_BF16 ? 2 : 4; }
+int32_t fail(int32_t code, const char *fmt, ...);
+int32_t check_stride(const char *name, const int64_t s[3], int dtype, int d);
+int32_t check_ptr(const char *name, const void *ptr, size_t align);
+int32_t check_ws(const void *ws, size_t have, size_t need);
+int32_t hip_result(hipError_t e, const char *what);
+
 // Geometry of one prefill call, passed by value to the kernels.
 struct ScoreGeom {
     const void *q, *k, *v;
@@ -231,5 +240,43 @@ struct DecodePlan {
 };
 hipError_t launch_decode(const DecodeGeom &g, const DecodePlan &pl, void *ws, int dtype,
                          hipStream_t st);
+
+// The paged tails of a batch: token s of sequence b in row s % 2^page_shift of page table[b][s >> page_shift].
+struct PageGeom {
+    int64_t ks[3], vs[3];  // element strides: page, head, row
+    const int32_t *table, *tail_len, *new_len;  // (new_len may be null: every row is real)
+    int n_pages, page_shift, table_width;
+};
+// rotate.hip
+// Rows of q and k turned by their positions; with `append` k and v go to their places in the pages.
+struct RotaryGeom {
+    const void *q, *k, *v;
+    void *q_out, *k_out, *v_out;  // (append: the pools)
+    int64_t qs[3], ks[3], vs[3], qo[3], ko[3];  // element strides: batch, head, token
+    PageGeom pages;
+    int batch, n, Hq, Hkv, d, dtype;  // Hq or Hkv 0: not given
+    int rot, n_axes;
+    bool neighbours, transpose, append;
+    const float *inv_freq;
+    const int32_t *pair_axis, *positions;
+};
+hipError_t launch_rotate(const RotaryGeom &g, hipStream_t st);
+// shared_attn.hip
+// Rows of the new tokens over the prefix that their sequences share and their own tails.
+struct SharedGeom {
+    const void *q, *kp, *vp, *kt, *vt;  // prefixes; pools of the tails (null: none)
+    void *out;
+    float *lse;
+    const int32_t *prefix_len, *prefix_first;
+    int64_t qs[3], os[3], ks[3], vs[3];  // element strides: batch (prefix), head, token
+    PageGeom pages;
+    int batch, n, Hq, Hkv, G, d, dtype;  // n: rows per sequence and head
+    int n_prefixes, prefix_cap;
+    float scale;
+};
+struct SharedPlan {
+    size_t bytes;
+};
+hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &pl, void *ws, hipStream_t st);
 
 }  // namespace aha

@@ -1,0 +1,185 @@
+// Rotation of query and key rows by their positions, and its use in appending to a paged cache.
+//
+// Pair (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t) with t = position x frequency: three operations per
+// element read and written, so the bytes bound it.  What keeps the angles off that path: a thread owns the same
+// sixteen-byte chunks of a token's row in all heads, forms the sines and cosines of its eight pairs (fp32: four) once, while the
+// first heads' rows travel, and then goes through the heads.  Positions may be far (2^31) and the frequency 1: the
+// angle is formed in turns in double, its whole turns taken away there, and only the rest, at most half a
+// turn, becomes an fp32 number (off by 2^-26 of a turn at most, 1e-7 of the result).
+#include <algorithm>
+
+#include "aha_dev.h"
+#include "aha_host.h"
+
+namespace aha {
+
+// A row of d channels as D / CE chunks of 16 bytes, two of them per thread: of the rotated channels those whose elements
+// make pairs, of the others two neighbours.
+template <class T>
+struct RowChunks {
+    static constexpr int CE = 16 / sizeof(T);  // elements of a chunk, pairs of a thread
+    int first, second;
+    bool turned;
+    __device__ __forceinline__ RowChunks(int c, int rot, bool neighbours) {
+        const int np = rot / (2 * CE);  // threads with pairs
+        turned = c < np;
+        first = turned && !neighbours ? c : 2 * c;
+        second = turned && !neighbours ? c + np : 2 * c + 1;
+    }
+};
+
+__device__ __forceinline__ void unpack(const u32x4 &w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
+}
+__device__ __forceinline__ void unpack(const u32x4 &w, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ u32x4 pack(const float (&x)[8]) {
+    __bf16 b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = (__bf16)x[i];
+    u32x4 w;
+    __builtin_memcpy(&w, b, 16);
+    return w;
+}
+__device__ __forceinline__ u32x4 pack(const float (&x)[4]) {
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+}
+
+// The two chunks of a row, turned in place.
+template <class T, bool NEIGHBOURS>
+__device__ __forceinline__ void turn(u32x4 &w0, u32x4 &w1, const float (&cs)[RowChunks<T>::CE], const float (&sn)[RowChunks<T>::CE]) {
+    constexpr int CE = RowChunks<T>::CE;
+    float a[CE], b[CE];
+    unpack(w0, a);
+    unpack(w1, b);
+    if constexpr (NEIGHBOURS) {
+#pragma unroll
+        for (int i = 0; i < CE / 2; ++i) {
+            const float x = a[2 * i], y = a[2 * i + 1];
+            a[2 * i] = x * cs[i] - y * sn[i];
+            a[2 * i + 1] = x * sn[i] + y * cs[i];
+            const float u = b[2 * i], v = b[2 * i + 1];
+            b[2 * i] = u * cs[CE / 2 + i] - v * sn[CE / 2 + i];
+            b[2 * i + 1] = u * sn[CE / 2 + i] + v * cs[CE / 2 + i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < CE; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * cs[i] - y * sn[i];
+            b[i] = x * sn[i] + y * cs[i];
+        }
+    }
+    w0 = pack(a);
+    w1 = pack(b);
+}
+
+constexpr int kHeadsAhead = 4;  // rows of a thread in flight
+
+// A workgroup takes 256 / TPR tokens (TPR threads per row) and the heads [blockIdx.y * per, + per) of the Hq + Hkv (APPEND: +
+// Hkv value heads, which are copied).
+template <class T, int D, bool NEIGHBOURS, bool APPEND>
+__global__ __launch_bounds__(256) void rotate_kernel(RotaryGeom g, int per) {
+    constexpr int CE = RowChunks<T>::CE, TPR = D / (2 * CE), U = kHeadsAhead;
+    const int c = threadIdx.x % TPR;
+    const int64_t token = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    if (token >= (int64_t)g.batch * g.n) return;
+    const int b = (int)token / g.n, t = (int)token - b * g.n;
+    const int heads = g.Hq + (APPEND ? 2 : 1) * g.Hkv, h0 = blockIdx.y * per, h1 = min(heads, h0 + per);
+    const RowChunks<T> ch(c, g.rot, NEIGHBOURS);
+    int64_t k_at = 0, v_at = 0;  // APPEND: the token's row in the pools, without the head
+    bool placed = true;
+    if constexpr (APPEND) {
+        const int fresh = g.pages.new_len ? min(g.pages.new_len[b], g.n) : g.n;
+        if (t >= fresh) return;  // padding
+        const int64_t slot = (int64_t)g.pages.tail_len[b] - fresh + t, entry = slot >> g.pages.page_shift;
+        placed = slot >= 0 && entry < g.pages.table_width;
+        const int page = placed ? g.pages.table[(int64_t)b * g.pages.table_width + entry] : -1;
+        placed = page >= 0 && page < g.pages.n_pages;
+        const int row = (int)slot & ((1 << g.pages.page_shift) - 1);
+        k_at = page * g.pages.ks[0] + row * g.pages.ks[2];
+        v_at = page * g.pages.vs[0] + row * g.pages.vs[2];
+    }
+    auto source = [&](int h) {
+        const T *p = h < g.Hq            ? (const T *)g.q + b * g.qs[0] + h * g.qs[1] + t * g.qs[2]
+                     : h < g.Hq + g.Hkv  ? (const T *)g.k + b * g.ks[0] + (h - g.Hq) * g.ks[1] + t * g.ks[2]
+                                         : (const T *)g.v + b * g.vs[0] + (h - g.Hq - g.Hkv) * g.vs[1] + t * g.vs[2];
+        return p;
+    };
+    auto target = [&](int h) {
+        T *p = h < g.Hq           ? (T *)g.q_out + b * g.qo[0] + h * g.qo[1] + t * g.qo[2]
+               : !APPEND          ? (T *)g.k_out + b * g.ko[0] + (h - g.Hq) * g.ko[1] + t * g.ko[2]
+               : h < g.Hq + g.Hkv ? (T *)g.k_out + k_at + (h - g.Hq) * g.pages.ks[1]
+                                  : (T *)g.v_out + v_at + (h - g.Hq - g.Hkv) * g.pages.vs[1];
+        return p;
+    };
+    u32x4 w[U][2];
+    auto request = [&](int h) {  // (past the last head: that one again)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const T *p = source(min(h + u, h1 - 1));
+            w[u][0] = *(const u32x4 *)(p + ch.first * CE);
+            w[u][1] = *(const u32x4 *)(p + ch.second * CE);
+        }
+    };
+    request(h0);
+    float cs[CE], sn[CE];
+#pragma unroll
+    for (int i = 0; i < CE; ++i) cs[i] = 1.f, sn[i] = 0.f;
+    if (ch.turned) {
+#pragma unroll
+        for (int i = 0; i < CE; ++i) {
+            const int f = c * CE + i;
+            const int axis = g.pair_axis ? min(max(g.pair_axis[f], 0), g.n_axes - 1) : 0;
+            const int pos = g.positions[(int64_t)axis * g.batch * g.n + token];
+            double turns = (double)pos * ((double)g.inv_freq[f] * 0.15915494309189533577);
+            turns -= rint(turns);
+            sincospif(2.f * (float)turns, &sn[i], &cs[i]);
+            if (g.transpose) sn[i] = -sn[i];
+        }
+    }
+    for (int h = h0; h < h1; h += U) {
+        u32x4 x[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u][0] = w[u][0], x[u][1] = w[u][1];
+        if (h + U < h1) request(h + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (h + u >= h1) break;
+            const bool key = h + u >= g.Hq, value = APPEND && h + u >= g.Hq + g.Hkv;
+            if (ch.turned && !value) turn<T, NEIGHBOURS>(x[u][0], x[u][1], cs, sn);
+            if (key && !placed) continue;
+            T *p = target(h + u);
+            *(u32x4 *)(p + ch.first * CE) = x[u][0];
+            *(u32x4 *)(p + ch.second * CE) = x[u][1];
+        }
+    }
+}
+
+template <class T, int D, bool NEIGHBOURS, bool APPEND>
+static hipError_t launch_rotate_t(const RotaryGeom &g, hipStream_t st) {
+    constexpr int tokens = 256 * 2 * RowChunks<T>::CE / D;
+    const int64_t tiles = ((int64_t)g.batch * g.n + tokens - 1) / tokens;
+    const int heads = g.Hq + (APPEND ? 2 : 1) * g.Hkv, most = (heads + kHeadsAhead - 1) / kHeadsAhead;
+    // heads are dealt over workgroups, each of which forms the angles again, until 2048 workgroups have work (eight per CU)
+    const int64_t split = std::min<int64_t>(std::max<int64_t>(1, (2048 + tiles - 1) / tiles), most);
+    const int per = (int)((heads + split - 1) / split);
+    hipLaunchKernelGGL((rotate_kernel<T, D, NEIGHBOURS, APPEND>), dim3((unsigned)tiles, (heads + per - 1) / per), dim3(256), 0, st, g, per);
+    return hipGetLastError();
+}
+
+template <class T, int D>
+static hipError_t launch_rotate_d(const RotaryGeom &g, hipStream_t st) {
+    if (g.neighbours) return g.append ? launch_rotate_t<T, D, true, true>(g, st) : launch_rotate_t<T, D, true, false>(g, st);
+    return g.append ? launch_rotate_t<T, D, false, true>(g, st) : launch_rotate_t<T, D, false, false>(g, st);
+}
+
+hipError_t launch_rotate(const RotaryGeom &g, hipStream_t st) {
+    if (g.dtype == AHA_BF16) return g.d == 64 ? launch_rotate_d<__bf16, 64>(g, st) : launch_rotate_d<__bf16, 128>(g, st);
+    return g.d == 64 ? launch_rotate_d<float, 64>(g, st) : launch_rotate_d<float, 128>(g, st);
+}
+
+}  // namespace aha

@@ -1,0 +1,138 @@
+"""Attention behind shared prefixes (aha_shared_attention) against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests.shared_cases import Batch
+
+pytestmark = pytest.mark.gpu
+
+BOTH = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+
+
+@BOTH
+@pytest.mark.parametrize("d", [64, 128])
+def test_single_tokens(dtype, d):
+    Batch(1, q_heads=4, kv_heads=2, d=d, q_len=1, tail=[1, 7, 40, 16], prefix=[100], dtype=dtype).check()
+    Batch(2, q_heads=3, kv_heads=3, d=d, q_len=1, tail=[5], prefix=[1], page=1, dtype=dtype).check()
+    Batch(3, q_heads=8, kv_heads=1, d=d, q_len=1, tail=[33, 1, 130, 64, 65, 2, 31], prefix=[31, 257], first=[0, 3, 7],
+          page=32, dtype=dtype, layout="bnhd").check()
+    Batch(4, q_heads=14, kv_heads=2, d=d, q_len=1, tail=[100] * 11, prefix=[1000], page=64, dtype=dtype, hot=4.0).check()
+
+
+@BOTH
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunks(dtype, d):
+    Batch(5, q_heads=4, kv_heads=2, d=d, q_len=3, tail=[3, 10, 17], prefix=[65], dtype=dtype).check()
+    Batch(6, q_heads=4, kv_heads=2, d=d, q_len=33, tail=[40, 33, 200], new=[33, 20, 1], prefix=[300, 7], first=[0, 1, 3],
+          page=8, dtype=dtype, layout="bnhd").check()
+    Batch(7, q_heads=2, kv_heads=1, d=d, q_len=150, tail=[150, 700], new=[150, 149], prefix=[513], page=128, dtype=dtype).check()
+
+
+@BOTH
+def test_rows_without_keys_and_padding(dtype):
+    # no prefix for sequences 0 and 4, an empty prefix, tails without tokens, sequences without new rows
+    d = Batch(8, q_heads=4, kv_heads=2, d=64, q_len=2, tail=[0, 0, 9, 2, 0, 5], new=[2, 1, 2, 0, 2, 2], prefix=[0, 40],
+              first=[1, 2, 4], dtype=dtype).check()
+    assert torch.isneginf(d["lse"][0]).all()
+    # tails shorter than their new rows: the first rows come before token 0
+    Batch(9, q_heads=2, kv_heads=2, d=128, q_len=6, tail=[3, 0, 6], dtype=dtype).check()
+    Batch(10, q_heads=2, kv_heads=2, d=128, q_len=40, tail=[35, -4, 2], new=[40, 3, 40], prefix=[3], first=[2, 3], dtype=dtype).check()
+
+
+@BOTH
+def test_holes(dtype):
+    holes = {(0, 0): -1, (0, 2): 10 ** 6, (1, 1): -7, (2, 0): -1, (2, 1): -1, (2, 2): -1}
+    for page in (4, 16, 32, 64):
+        Batch(11, q_heads=4, kv_heads=2, d=128, q_len=2, tail=[3 * page, 2 * page + 1, 3 * page - 1], page=page, holes=holes,
+              prefix=[20], first=[0, 2], dtype=dtype).check()
+
+
+@BOTH
+def test_prefix_alone(dtype):
+    """Without tails: the attention of rows over an encoder's states, say."""
+    Batch(12, q_heads=4, kv_heads=4, d=64, q_len=19, tail=[0, 0], prefix=[77, 300], first=[0, 1, 2], dtype=dtype, tails=False).check()
+
+
+@BOTH
+def test_tails_alone(dtype):
+    Batch(13, q_heads=4, kv_heads=1, d=128, q_len=1, tail=[1, 300, 64, 999], page=16, dtype=dtype).check()
+
+
+def test_lengths_beyond_what_is_there_are_clamped():
+    b = Batch(14, q_heads=4, kv_heads=2, d=64, q_len=2, tail=[32, 10], new=[2, 2], prefix=[50], cap=50, page=16)
+    d = b.upload()
+    d["prefix"].fill_(2 ** 31 - 1)
+    d["new"].fill_(99)
+    d["first"].copy_(torch.tensor([0, 2 ** 31 - 1], dtype=torch.int32))
+    b.run(d)
+    b.check(d)
+    d["first"].copy_(torch.tensor([-2 ** 31, 2], dtype=torch.int32))
+    d["out"].fill_(float("nan"))
+    b.run(d)
+    b.check(d)
+
+
+def test_members_in_many_groups():
+    rng = np.random.default_rng(3)
+    batch = 37
+    first = np.sort(rng.integers(0, batch + 1, size=9)).tolist()
+    Batch(15, q_heads=6, kv_heads=2, d=64, q_len=1, tail=rng.integers(1, 90, batch).tolist(), prefix=rng.integers(0, 400, 8).tolist(),
+          first=first, page=16).check()
+
+
+def random_batch(seed):
+    rng = np.random.default_rng(seed)
+    log = lambda lo, hi: int(round(np.exp(rng.uniform(np.log(lo), np.log(hi)))))
+    f32 = rng.random() < 0.25
+    batch, hkv, group = log(1, 24), int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 3, 4, 7, 8]))
+    q_len = int(rng.choice([1, 1, log(2, 8), log(9, 140)]))
+    prefixes = int(rng.choice([0, 1, 1, 2, 5]))
+    prefix = [int(rng.choice([0, log(1, 60), log(60, 3000)])) for _ in range(prefixes)]
+    new = rng.integers(0, q_len + 1, batch) if rng.random() < 0.5 else np.full(batch, q_len)
+    tail = new + [log(1, 500) - 1 for _ in range(batch)]
+    page = int(rng.choice([1, 4, 16, 32, 64, 256]))
+    width = -(-int(max(tail.max(), 1)) // page)
+    holes = {(int(rng.integers(batch)), int(rng.integers(width))): int(rng.choice([-1, 10 ** 6])) for _ in range(rng.integers(0, 6))}
+    first = np.sort(rng.integers(0, batch + 1, prefixes + 1)).tolist() if prefixes else None
+    return Batch(seed, q_heads=hkv * group, kv_heads=hkv, d=int(rng.choice([64, 128])), q_len=q_len, tail=tail.tolist(),
+                 new=new.tolist() if rng.random() < 0.8 or (new < q_len).any() else None, prefix=prefix, first=first, page=page, holes=holes,
+                 cap=max(prefix + [1]) + int(rng.integers(0, 50)), dtype=torch.float32 if f32 else torch.bfloat16,
+                 layout=str(rng.choice(["bhnd", "bnhd"])), scale=None if rng.random() < 0.8 else float(rng.choice([0.0, 0.3])),
+                 hot=float(rng.choice([0.0, 3.0])))
+
+
+@pytest.mark.parametrize("block", range(6))
+def test_random_batches(block):
+    for seed in range(100 + 10 * block, 110 + 10 * block):
+        print("seed", seed, end=" ", flush=True)
+        random_batch(seed).check()
+
+
+@BOTH
+def test_logits_that_keep_rising(dtype):
+    """Keys that grow along the queries' direction: the running maximum moves in every step, in small
+    and in large ones."""
+    for slope in (0.02, 0.3):
+        b = Batch(16, q_heads=8, kv_heads=2, d=64, q_len=2, tail=[300, 200], prefix=[1500], page=16, dtype=dtype)
+        u = torch.randn(64, generator=torch.Generator().manual_seed(1)).to(dtype)
+        b.q += u
+        for t in (b.kp, b.kt):
+            t += (torch.arange(t.size(2))[None, None, :, None] * slope * u / 8).to(dtype)
+        b.check()
+
+
+def test_without_lse_and_in_strided_outputs():
+    b = Batch(17, q_heads=4, kv_heads=2, d=128, q_len=5, tail=[20, 9], prefix=[200])
+    d = b.upload()
+    b.run(d)
+    wide = torch.full((2, 4, 5, 3 * 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    dense = d["out"].clone()
+    from paper_2506_03762_amd import binding as B
+    d["out"] = wide[..., 128:256]
+    d["p"] = B.SharedAttention.of(d["q"], d["out"], d["kp"], d["vp"], b.scale)
+    d["ws"].fill_(0x5A)
+    b.run(d, lse=False)
+    torch.cuda.synchronize()
+    assert torch.equal(d["out"], dense)
+    assert torch.isnan(wide[..., :128].float()).all() and torch.isnan(wide[..., 256:].float()).all()
