@@ -274,7 +274,13 @@ struct SharedGeom {
     int n_prefixes, prefix_cap;
     float scale;
 };
+// Work items: tiles of rows (prefixes: an upper bound, the sequences of each are known on the device) times KV heads (and sequences)
+// times parts of the keys; what lies where in the workspace.
 struct SharedPlan {
+    int prefix_tiles, prefix_parts, tail_tiles, tail_parts;
+    int64_t prefix_items, tail_items;
+    float c_out;    // scale times log2(e), above 0
+    size_t off_ms;  // (reference, sum) pairs behind the partial outputs
     size_t bytes;
 };
 hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &pl, void *ws, hipStream_t st);

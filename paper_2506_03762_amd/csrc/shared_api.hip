@@ -2,6 +2,8 @@
 // that shares prefixes.  All checks run on the host before anything is enqueued.
 #include <math.h>
 
+#include <algorithm>
+
 #include "aha_host.h"
 
 namespace aha {
@@ -122,9 +124,39 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
     return check_stride("v", p->v_stride, p->dtype, p->head_dim);
 }
 
-static SharedPlan plan_shared(const aha_shared *, const aha_pages *) {
+// Parts of an item's keys: as many as give the chip 512 workgroups (two per CU) with `tiles` in each, of two steps at least.
+static int64_t parts_for(int64_t tiles, int64_t keys, int step) {
+    const int64_t steps = (keys + step - 1) / step;
+    return std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, (steps + 1) / 2, 64}));
+}
+static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {
     SharedPlan pl{};
+    const int64_t per = (int64_t)(p->n_q_heads / p->n_kv_heads) * p->q_len, all = per * p->batch;
+    const int64_t tile = 32, step = 128;
+    if (p->n_prefixes > 0) {
+        const int64_t members = std::min<int64_t>(p->n_prefixes, p->batch);  // prefixes with rows, each with a last tile that is not full
+        const int64_t tiles = (all + members * (tile - 1)) / tile, parts = parts_for(tiles * p->n_kv_heads, p->prefix_cap, step);
+        pl.prefix_tiles = (int)tiles;
+        pl.prefix_parts = (int)parts;
+        pl.prefix_items = (p->n_kv_heads * parts + 7) / 8 * 8 * tiles;
+    }
+    if (pages) {
+        const int64_t tiles = (per + tile - 1) / tile, units = (int64_t)p->batch * p->n_kv_heads;
+        const int64_t parts = parts_for(tiles * units, (int64_t)pages->table_width * pages->page_size, step);
+        pl.tail_tiles = (int)tiles;
+        pl.tail_parts = (int)parts;
+        pl.tail_items = (units * parts + 7) / 8 * 8 * tiles;
+    }
+    pl.c_out = std::max((float)(p->scale * 1.4426950408889634), 1e-37f);
+    const size_t rows = (size_t)all * p->n_kv_heads * (pl.prefix_parts + pl.tail_parts);
+    pl.off_ms = align_up(sizeof(float) * rows * p->head_dim, 256);
+    pl.bytes = align_up(pl.off_ms + 2 * sizeof(float) * rows, 256);
     return pl;
+}
+
+static int32_t check_items(const SharedPlan &pl) {
+    if (pl.prefix_items + pl.tail_items > 1 << 30) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
+    return AHA_OK;
 }
 
 }  // namespace aha
@@ -176,9 +208,11 @@ int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void
 
 int32_t aha_shared_attention_workspace_bytes(const aha_shared *p, const aha_pages *pages, size_t *out_bytes) {
     if (!out_bytes) return fail(AHA_ERR_INVALID_ARG, "out_bytes is null");
-    const int32_t rc = check_shared(p, pages, false);
+    int32_t rc = check_shared(p, pages, false);
     if (rc) return rc;
-    *out_bytes = plan_shared(p, pages).bytes;
+    const SharedPlan pl = plan_shared(p, pages);
+    if ((rc = check_items(pl))) return rc;
+    *out_bytes = pl.bytes;
     return AHA_OK;
 }
 
@@ -202,6 +236,7 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
         return fail(AHA_ERR_INVALID_ARG, "pages is null, but tails are given");
     }
     const SharedPlan pl = plan_shared(p, pages);
+    if ((rc = check_items(pl))) return rc;
     if ((rc = check_ws(workspace, workspace_bytes, pl.bytes))) return rc;
     SharedGeom g{};
     g.q = q; g.kp = k_prefix; g.vp = v_prefix; g.kt = k_pages; g.vt = v_pages; g.out = out; g.lse = lse;

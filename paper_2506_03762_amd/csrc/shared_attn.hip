@@ -1,110 +1,379 @@
 // Attention of a batch's new tokens over the prefixes that its sequences share and over their own tails in pages.
-#include "aha_dev.h"
-#include "aha_host.h"
+//
+//   out = sum_j softmax_j(scale q . K_j) V_j
+//
+// in parts: a work item (shared_rows.h) forms sum_j 2^(x_j - m) V_j, sum_j 2^(x_j - m) and m over its keys, x = scale log2(e) q . K, in
+// one pass with a running reference m; a row's parts are joined by a second launch.  A prefix's keys are read once for a tile of
+// rows of all its sequences, which is what makes the products of a batch matrix products.
+#include <limits.h>
+
+#include "f32_tile.h"
+#include "shared_rows.h"
+#include "value_rows.h"
 
 namespace aha {
 
-// The keys of a sequence's row: prefix tokens [0, ahead), then tail tokens [0, behind).
-struct RowKeys {
-    int prefix, ahead, behind;
+constexpr float kRefSlack = 8.f;  // log2 units that a reference may lie below the running maximum
+constexpr float kLn2 = 0.69314718055994531f;
+
+// ---- bf16, up to 32 rows ----
+// Four waves take blocks of 32 keys in turn, each with all rows: a stream of keys and values, bound by memory.  Per block and
+// wave: S^T = K Q^T and O^T += V^T P^T by v_mfma_f32_32x32x16_bf16, keys (channels) on M, rows on N, so that the accumulator elements of a
+// lane are the probabilities that it supplies to the second product.  Keys go to registers, values to LDS, both a block ahead.
+template <int D>
+struct NarrowAttn {
+    static constexpr int WAVES = 4, STEP = 32 * WAVES, CPR = D / 8, RPI = 64 / CPR, NI = 32 / RPI;
+    static constexpr int HC = D / 2, LDO = HC + 1;  // channels per pass of the waves' merge, floats of a row there
+    static constexpr size_t v_bytes = 32 * D * 2;   // a block's value rows
+    static constexpr size_t o_bytes = (size_t)WAVES * 32 * LDO * 4, merge_bytes = o_bytes + (size_t)WAVES * 32 * 8;
+    static constexpr size_t stage_bytes = 2 * WAVES * v_bytes;
+    static constexpr size_t bytes = stage_bytes > merge_bytes ? stage_bytes : merge_bytes;
 };
-__device__ __forceinline__ RowKeys row_keys(const SharedGeom &g, int b, int t, int fresh) {
-    RowKeys r{-1, 0, 0};
-    int lo = 0, hi = g.n_prefixes;  // the last prefix that begins at or before b
+template <int D>
+__global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
+    using A = NarrowAttn<D>;
+    constexpr int KS = D / 16, CB = D / 32;
+    __shared__ __attribute__((aligned(1024))) char smem[A::bytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    SharedItem it;
+    if (!shared_item(g, pl, (int)blockIdx.x, 32, A::STEP, lane, it)) return;
+    const SharedRow row(g, it, it.row0 + col);
+    if (it.begin >= it.end) {  // no keys in this part
+        if (tid < 32 && row.live) part_ms[partial_index(g, pl, it.h, it.part, it.row0 + tid)] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    const SharedKeys<__bf16> keys(g, it);
+    bf16x8 qf[KS];
+    {
+        const __bf16 *p = (const __bf16 *)g.q + row.b * g.qs[0] + row.hq * g.qs[1] + row.t * g.qs[2] + hf * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks] = *(const bf16x8 *)(p + ks * 16);
+            if (!row.live) qf[ks] = bf16x8{};
+        }
+    }
+    const float c_out = pl.c_out;
+    const int limit = row.limit, limit_min = -reduce_lanes<1, 32>(-limit, OpMaxI{});
+
+    // Value rows of a block -> LDS, chunks permuted on the way (value_rows.h); loads are assembly, waited for by hand.
+    const uint32_t lds0 = uniform((int)((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem + wave * 2 * (int)A::v_bytes));
+    const int lr = lane / A::CPR, chunk = (lane % A::CPR) ^ value_chunk_swizzle<D>(lr);
+    auto request_values = [&](const __bf16 *v, int buf) {  // v: this lane's row lane % 32
+        const uint64_t mine = (uint64_t)(uintptr_t)v;
+#pragma unroll
+        for (int j = 0; j < A::NI; ++j) {
+            const int from = j * A::RPI + lr;
+            const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
+            const uint64_t src = (((uint64_t)hi << 32) | lo) + chunk * 16;
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                         :
+                         : "v"(src), "s"(lds0 + buf * (int)A::v_bytes + j * 1024)
+                         : "memory");
+        }
+    };
+    bf16x8 a[KS];
+    auto load_keys = [&](const __bf16 *k) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) a[ks] = *(const bf16x8 *)(k + hf * 8 + ks * 16);
+    };
+
+    f32x16 O[CB];
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) O[cb][v] = 0.f;
+    int kb = it.begin + wave * 32;
+    int next_entry = keys.entry(kb + A::STEP + col);
+    auto here = keys.at(kb + col, keys.entry(kb + col));
+    request_values(here.v, 0);
+    load_keys(here.k);
+    for (int buf = 0; kb < it.end; kb += A::STEP, buf ^= 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        wait_loads<0>();                                   // this block's keys and values are here,
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // and the last block's values have been read
+        const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(here.there);  // (lanes 0 .. 31)
+        here = keys.at(kb + A::STEP + col, next_entry);
+        next_entry = keys.entry(kb + 2 * A::STEP + col);
+        request_values(here.v, buf ^ 1);
+        f32x16 acc;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], qf[ks], acc, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(here.k);
+        __builtin_amdgcn_sched_barrier(0);
+        if (there != 0xffffffffu || kb + 31 > limit_min) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int at = 8 * (v >> 2) + 4 * hf + (v & 3);
+                if (kb + at > limit || !((there >> at) & 1)) acc[v] = -INFINITY;
+            }
+        }
+        float amax = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) amax = fmaxf(amax, acc[v]);
+        amax = combine_lane_xor<32>(amax, OpMax{});
+        // (the reference follows the running maximum lazily: it moves when a block's exceeds it by more than kRefSlack)
+        const float bm = amax * c_out;
+        const float mn = bm > m + kRefSlack ? bm : m;
+        const float mref = mn == -INFINITY ? 0.f : mn;
+        const float corr = fast_exp2(m - mref);
+        float sum[2] = {0.f, 0.f};
+        bf16x8 pf[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float pr = fast_exp2(fmaf(acc[8 * ks + e], c_out, -mref));
+                sum[e & 1] += pr;
+                pf[ks][e] = (__bf16)pr;
+            }
+        s = s * corr + (sum[0] + sum[1]);
+        m = mn;
+        if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
+        }
+        const __bf16 *sV = (const __bf16 *)(smem + (wave * 2 + buf) * A::v_bytes);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_fragment<D>(sV, 0, ks, cb, lane), pf[ks], O[cb], 0, 0, 0);
+    }
+    wait_loads<0>();
+
+    // ---- the waves' partials meet in LDS, half of the channels at a time ----
+    __syncthreads();
+    float2 *sMS = (float2 *)(smem + A::o_bytes);
+    const float sc = combine_lane_xor<32>(s, OpSum{});
+    if (lane < 32) sMS[wave * 32 + lane] = make_float2(m, sc);
+    const int rows = it.row1 - it.row0;
+    const uint32_t live = (uint32_t)__builtin_amdgcn_ballot_w64(row.live);
+#pragma unroll
+    for (int hc = 0; hc < 2; ++hc) {
+        float *sO = (float *)smem + wave * 32 * A::LDO;
+        if (hc) __syncthreads();
+#pragma unroll
+        for (int cb = 0; cb < CB / 2; ++cb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (col < rows) sO[col * A::LDO + cb * 32 + 8 * (v >> 2) + 4 * hf + (v & 3)] = O[hc * (CB / 2) + cb][v];
+        __syncthreads();
+        for (int i = tid; i < rows * A::HC; i += 256) {
+            const int q = i / A::HC, ch = i % A::HC;
+            if (!((live >> q) & 1)) continue;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < A::WAVES; ++w) M = fmaxf(M, sMS[w * 32 + q].x);
+            const float mref = M == -INFINITY ? 0.f : M;
+            float o = 0.f, ssum = 0.f;
+#pragma unroll
+            for (int w = 0; w < A::WAVES; ++w) {
+                const float2 ms = sMS[w * 32 + q];
+                const float f = fast_exp2(ms.x - mref);
+                o = fmaf(f, ((const float *)smem)[(w * 32 + q) * A::LDO + ch], o);
+                ssum = fmaf(f, ms.y, ssum);
+            }
+            const int64_t p = partial_index(g, pl, it.h, it.part, it.row0 + q);
+            part_o[p * D + hc * A::HC + ch] = o;
+            if (hc == 0 && ch == 0) part_ms[p] = make_float2(M, ssum);
+        }
+    }
+}
+
+// ---- fp32 ----
+// The same on v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it): a lane's chunks of a key row and a query
+// row as in f32_tile.h; the second product takes the probabilities from the accumulators one element at a time, a
+// contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.
+template <int D>
+struct F32Attn {
+    static constexpr int WAVES = 4, STEP = 32 * WAVES, HC = D / 2, LDO = HC + 1, LDQ = f32_ld(D);
+    static constexpr size_t o_bytes = (size_t)WAVES * 32 * LDO * 4, q_bytes = (size_t)32 * LDQ * 4;
+    static constexpr size_t bytes = (o_bytes > q_bytes ? o_bytes : q_bytes) + (size_t)WAVES * 32 * 8;
+};
+template <int D>
+__global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
+    using A = F32Attn<D>;
+    constexpr int CB = D / 32;
+    __shared__ __attribute__((aligned(16))) char smem[A::bytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    SharedItem it;
+    if (!shared_item(g, pl, (int)blockIdx.x, 32, A::STEP, lane, it)) return;
+    const SharedRow row(g, it, it.row0 + col);
+    if (it.begin >= it.end) {
+        if (tid < 32 && row.live) part_ms[partial_index(g, pl, it.h, it.part, it.row0 + tid)] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    const SharedKeys<float> keys(g, it);
+    float *sQ = (float *)smem;
+    {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
+        const float *p = (const float *)g.q + row.b * g.qs[0] + row.hq * g.qs[1] + row.t * g.qs[2];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const int c = wave * (D / 4) + i * 8 + hf * 4;
+            f32x4 x = *(const f32x4 *)(p + c);
+            if (!row.live) x = f32x4{};
+            *(f32x4 *)(sQ + col * A::LDQ + c) = x;
+        }
+    }
+    __syncthreads();
+    const float *sq = sQ + col * A::LDQ + 4 * hf;
+    const float c_out = pl.c_out;
+    const int limit = row.limit, limit_min = -reduce_lanes<1, 32>(-limit, OpMaxI{});
+    f32x16 O[CB];
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) O[cb][v] = 0.f;
+    for (int kb = it.begin + wave * 32; kb < it.end; kb += A::STEP) {
+        const auto here = keys.at(kb + col, keys.entry(kb + col));
+        const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(here.there);
+        f32x4 a[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) a[i] = *(const f32x4 *)(here.k + 4 * hf + 8 * i);
+        f32x16 acc = f32_block_dots<D>(a, sq);
+        if (there != 0xffffffffu || kb + 31 > limit_min) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int at = 8 * (v >> 2) + 4 * hf + (v & 3);
+                if (kb + at > limit || !((there >> at) & 1)) acc[v] = -INFINITY;
+            }
+        }
+        float amax = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) amax = fmaxf(amax, acc[v]);
+        amax = combine_lane_xor<32>(amax, OpMax{});
+        const float mn = fmaxf(m, amax * c_out);
+        const float mref = mn == -INFINITY ? 0.f : mn;
+        const float corr = fast_exp2(m - mref);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            acc[v] = fast_exp2(fmaf(acc[v], c_out, -mref));
+            sum[v & 3] += acc[v];
+        }
+        s = s * corr + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        m = mn;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
+        const uint64_t mine = (uint64_t)(uintptr_t)here.v;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int from = 8 * (v >> 2) + 4 * hf + (v & 3);
+            const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
+            const float *vr = (const float *)(((uint64_t)hi << 32) | lo) + col;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) O[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[cb * 32], acc[v], O[cb], 0, 0, 0);
+        }
+    }
+    __syncthreads();  // the query rows are done with
+    float2 *sMS = (float2 *)(smem + A::bytes - (size_t)A::WAVES * 32 * 8);
+    const float sc = combine_lane_xor<32>(s, OpSum{});
+    if (lane < 32) sMS[wave * 32 + lane] = make_float2(m, sc);
+    const int rows = it.row1 - it.row0;
+    const uint32_t live = (uint32_t)__builtin_amdgcn_ballot_w64(row.live);
+#pragma unroll
+    for (int hc = 0; hc < 2; ++hc) {
+        float *sO = (float *)smem + wave * 32 * A::LDO;
+        if (hc) __syncthreads();
+#pragma unroll
+        for (int cb = 0; cb < CB / 2; ++cb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (col < rows) sO[col * A::LDO + cb * 32 + 8 * (v >> 2) + 4 * hf + (v & 3)] = O[hc * (CB / 2) + cb][v];
+        __syncthreads();
+        for (int i = tid; i < rows * A::HC; i += 256) {
+            const int q = i / A::HC, ch = i % A::HC;
+            if (!((live >> q) & 1)) continue;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < A::WAVES; ++w) M = fmaxf(M, sMS[w * 32 + q].x);
+            const float mref = M == -INFINITY ? 0.f : M;
+            float o = 0.f, ssum = 0.f;
+#pragma unroll
+            for (int w = 0; w < A::WAVES; ++w) {
+                const float2 ms = sMS[w * 32 + q];
+                const float f = fast_exp2(ms.x - mref);
+                o = fmaf(f, ((const float *)smem)[(w * 32 + q) * A::LDO + ch], o);
+                ssum = fmaf(f, ms.y, ssum);
+            }
+            const int64_t p = partial_index(g, pl, it.h, it.part, it.row0 + q);
+            part_o[p * D + hc * A::HC + ch] = o;
+            if (hc == 0 && ch == 0) part_ms[p] = make_float2(M, ssum);
+        }
+    }
+}
+
+// ---- joining a row's parts ----
+// A thread takes four channels of a row.  Parts without a key have a reference of -inf and no output; rows without a prefix have no
+// prefix parts.
+template <class T, int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedGeom g, SharedPlan pl, const float *part_o, const float2 *part_ms) {
+    constexpr int TPR = D / 4;
+    const int per = rows_of_sequence(g), row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
+    if (row >= g.batch * per) return;
+    const int h = blockIdx.y, b = row / per, at = row - b * per, gi = at / g.n, t = at - gi * g.n;
+    if (t >= fresh_of(g, b)) return;
+    int lo = 0, hi = g.n_prefixes;  // prefixes that begin at or before b
     while (lo < hi) {
         const int mid = (lo + hi) / 2;
-        if (g.prefix_first[mid] <= b) lo = mid + 1; else hi = mid;
+        if (first_of(g, mid) <= b) lo = mid + 1; else hi = mid;
     }
-    if (lo > 0 && b < g.prefix_first[lo]) {
-        r.prefix = lo - 1;
-        r.ahead = min(max(g.prefix_len[r.prefix], 0), g.prefix_cap);
+    const bool ahead = lo > 0 && b < first_of(g, lo);
+    const int p0 = ahead ? 0 : pl.prefix_parts, p1 = pl.prefix_parts + pl.tail_parts;
+    float M = -INFINITY, ssum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int p = p0; p < p1; ++p) {
+        const int64_t i = partial_index(g, pl, h, p, row);
+        const float2 ms = part_ms[i];
+        if (ms.x == -INFINITY) continue;
+        const f32x4 x = *(const f32x4 *)(part_o + i * D + ch);
+        const float mn = fmaxf(M, ms.x), f0 = exp2f(M - mn), f1 = exp2f(ms.x - mn);
+        ssum = ssum * f0 + f1 * ms.y;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = o[c] * f0 + f1 * x[c];
+        M = mn;
     }
-    if (g.kt) {
-        const int64_t seen = (int64_t)g.pages.tail_len[b] - fresh + t + 1;
-        r.behind = (int)max((int64_t)0, min(seen, (int64_t)g.pages.table_width << g.pages.page_shift));
+    const float inv = ssum == 0.f ? 0.f : 1.f / ssum;
+    T *out = (T *)g.out + b * g.os[0] + (h * g.G + gi) * g.os[1] + t * g.os[2] + ch;
+    if constexpr (sizeof(T) == 2) {
+        *(uint2 *)out = uint2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+    } else {
+        *(f32x4 *)out = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
     }
-    return r;
+    if (g.lse && ch == 0) g.lse[((int64_t)b * g.Hq + h * g.G + gi) * g.n + t] = ssum == 0.f ? -INFINITY : (M + log2f(ssum)) * kLn2;
 }
 
-// A workgroup per row; keys in blocks of 256, one per thread, then a channel per thread.
 template <class T, int D>
-__global__ __launch_bounds__(256) void shared_attn_kernel(SharedGeom g) {
-    constexpr int SL = 256 / D, CE = 16 / sizeof(T);
-    const int rows = g.G * g.n, b = blockIdx.x / rows, rr = blockIdx.x % rows, gi = rr / g.n, t = rr % g.n;
-    const int h = blockIdx.y, hq = h * g.G + gi, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int fresh = g.pages.new_len ? min(max(g.pages.new_len[b], 0), g.n) : g.n;
-    if (t >= fresh) return;
-    const RowKeys rk = row_keys(g, b, t, fresh);
-    const int64_t keys = (int64_t)rk.ahead + rk.behind;
-    __shared__ float s_q[D], s_p[256], s_red[4], s_o[SL][D];
-    __shared__ const T *s_v[256];
-    if (tid < D) s_q[tid] = (float)((const T *)g.q + b * g.qs[0] + hq * g.qs[1] + t * g.qs[2])[tid];
-    __syncthreads();
-    const float c_out = g.scale * kLog2e;
-    const int c = tid % D, sl = tid / D;
-    float m = -INFINITY, ssum = 0.f, o = 0.f;
-    for (int64_t j0 = 0; j0 < keys; j0 += 256) {
-        const int64_t j = j0 + tid;
-        const T *kr = nullptr, *vr = nullptr;
-        if (j < rk.ahead) {
-            kr = (const T *)g.kp + rk.prefix * g.ks[0] + h * g.ks[1] + j * g.ks[2];
-            vr = (const T *)g.vp + rk.prefix * g.vs[0] + h * g.vs[1] + j * g.vs[2];
-        } else if (j < keys) {
-            const int s = (int)(j - rk.ahead), row = s & ((1 << g.pages.page_shift) - 1);
-            const int page = g.pages.table[(int64_t)b * g.pages.table_width + (s >> g.pages.page_shift)];
-            if (page >= 0 && page < g.pages.n_pages) {
-                kr = (const T *)g.kt + page * g.pages.ks[0] + h * g.pages.ks[1] + row * g.pages.ks[2];
-                vr = (const T *)g.vt + page * g.pages.vs[0] + h * g.pages.vs[1] + row * g.pages.vs[2];
-            }
-        }
-        float x = -INFINITY;
-        if (kr) {
-            float w = 0.f;
-            for (int cc = 0; cc < D / CE; ++cc) {
-                T e[CE];
-                __builtin_memcpy(e, kr + cc * CE, 16);
-                for (int i = 0; i < CE; ++i) w = fmaf(s_q[cc * CE + i], (float)e[i], w);
-            }
-            x = w * c_out;
-        }
-        const float wm = wave_max(x);
-        if (lane == 0) s_red[wave] = wm;
-        __syncthreads();
-        const float mn = fmaxf(m, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-        const float mref = mn == -INFINITY ? 0.f : mn;
-        const float pr = exp2f(x - mref);
-        s_p[tid] = pr;
-        s_v[tid] = vr;
-        const float ws = wave_sum(pr);
-        __syncthreads();
-        if (lane == 0) s_red[wave] = ws;
-        __syncthreads();
-        const float corr = exp2f(m - mref);
-        ssum = ssum * corr + (s_red[0] + s_red[1] + s_red[2] + s_red[3]);
-        o *= corr;
-        for (int jj = sl; jj < 256; jj += SL)
-            if (s_v[jj]) o = fmaf(s_p[jj], (float)s_v[jj][c], o);
-        m = mn;
-        __syncthreads();
+static hipError_t launch_shared_t(const SharedGeom &g, const SharedPlan &pl, void *ws, hipStream_t st) {
+    float *part_o = (float *)ws;
+    float2 *part_ms = (float2 *)((char *)ws + pl.off_ms);
+    const int64_t items = pl.prefix_items + pl.tail_items;
+    if (items > 0) {
+        if constexpr (sizeof(T) == 2)
+            hipLaunchKernelGGL(shared_narrow_kernel<D>, dim3((unsigned)items), dim3(256), 0, st, g, pl, part_o, part_ms);
+        else
+            hipLaunchKernelGGL(shared_f32_kernel<D>, dim3((unsigned)items), dim3(256), 0, st, g, pl, part_o, part_ms);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    s_o[sl][c] = o;
-    __syncthreads();
-    if (tid < D) {
-        float tot = 0.f;
-        for (int t2 = 0; t2 < SL; ++t2) tot += s_o[t2][tid];
-        ((T *)g.out + b * g.os[0] + hq * g.os[1] + t * g.os[2])[tid] = (T)(ssum == 0.f ? 0.f : tot / ssum);
-        if (g.lse && tid == 0)
-            g.lse[((int64_t)b * g.Hq + hq) * g.n + t] = ssum == 0.f ? -INFINITY : (m + log2f(ssum)) * 0.69314718055994531f;
-    }
+    constexpr int rows = 1024 / D;
+    const int total = g.batch * g.G * g.n;
+    hipLaunchKernelGGL((shared_join_kernel<T, D>), dim3((unsigned)((total + rows - 1) / rows), g.Hkv), dim3(256), 0, st, g, pl, part_o, part_ms);
+    return hipGetLastError();
 }
 
-hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &, void *, hipStream_t st) {
-    const dim3 grid((unsigned)(g.batch * g.G * g.n), g.Hkv);
-    if (g.dtype == AHA_BF16 && g.d == 64) hipLaunchKernelGGL((shared_attn_kernel<__bf16, 64>), grid, dim3(256), 0, st, g);
-    else if (g.dtype == AHA_BF16) hipLaunchKernelGGL((shared_attn_kernel<__bf16, 128>), grid, dim3(256), 0, st, g);
-    else if (g.d == 64) hipLaunchKernelGGL((shared_attn_kernel<float, 64>), grid, dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((shared_attn_kernel<float, 128>), grid, dim3(256), 0, st, g);
-    return hipGetLastError();
+hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &pl, void *ws, hipStream_t st) {
+    if (g.dtype == AHA_BF16) return g.d == 64 ? launch_shared_t<__bf16, 64>(g, pl, ws, st) : launch_shared_t<__bf16, 128>(g, pl, ws, st);
+    return g.d == 64 ? launch_shared_t<float, 64>(g, pl, ws, st) : launch_shared_t<float, 128>(g, pl, ws, st);
 }
 
 }  // namespace aha
