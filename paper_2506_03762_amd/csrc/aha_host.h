@@ -277,12 +277,16 @@ struct SharedGeom {
 // Work items: tiles of rows (prefixes: an upper bound, the sequences of each are known on the device) times KV heads (and sequences)
 // times parts of the keys; what lies where in the workspace.
 struct SharedPlan {
-    int prefix_tiles, prefix_parts, tail_tiles, tail_parts;
+    int prefix_rows, prefix_tiles, prefix_parts;  // rows of a tile: 32, or 128 or 256 (shared_wide.hip)
+    int tail_rows, tail_tiles, tail_parts;
     int64_t prefix_items, tail_items;
     float c_out;    // scale times log2(e), above 0
     size_t off_ms;  // (reference, sum) pairs behind the partial outputs
     size_t bytes;
 };
 hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &pl, void *ws, hipStream_t st);
+// shared_wide.hip
+// The items of `pl` in tiles of 128 or 256 rows (bf16).
+hipError_t launch_shared_wide(const SharedGeom &g, const SharedPlan &pl, int rows, float *part_o, float2 *part_ms, hipStream_t st);
 
 }  // namespace aha

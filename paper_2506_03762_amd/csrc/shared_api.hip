@@ -124,25 +124,30 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
     return check_stride("v", p->v_stride, p->dtype, p->head_dim);
 }
 
-// Parts of an item's keys: as many as give the chip 512 workgroups (two per CU) with `tiles` in each, of two steps at least.
-static int64_t parts_for(int64_t tiles, int64_t keys, int step) {
-    const int64_t steps = (keys + step - 1) / step;
-    return std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, (steps + 1) / 2, 64}));
+// Rows of a tile for about `rows` rows that see the same keys.
+static int tile_rows(int dtype, int64_t rows) { return dtype != AHA_BF16 || rows <= 64 ? 32 : rows <= 128 ? 128 : 256; }
+// Parts of an item's keys: as many as fill the chip (two workgroups per CU, large tiles one) with `tiles` in each, of two steps at
+// least (large tiles four).
+static int64_t parts_for(int64_t tiles, int64_t keys, int rows) {
+    const int64_t step = rows > 32 ? 64 : 128, steps = (keys + step - 1) / step, resident = rows > 32 ? 256 : 512, least = rows > 32 ? 4 : 2;
+    return std::max<int64_t>(1, std::min<int64_t>({(resident + tiles - 1) / tiles, (steps + least - 1) / least, 64}));
 }
 static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {
     SharedPlan pl{};
     const int64_t per = (int64_t)(p->n_q_heads / p->n_kv_heads) * p->q_len, all = per * p->batch;
-    const int64_t tile = 32, step = 128;
+    pl.tail_rows = tile_rows(p->dtype, per);
+    pl.prefix_rows = pl.tail_rows;
     if (p->n_prefixes > 0) {
-        const int64_t members = std::min<int64_t>(p->n_prefixes, p->batch);  // prefixes with rows, each with a last tile that is not full
-        const int64_t tiles = (all + members * (tile - 1)) / tile, parts = parts_for(tiles * p->n_kv_heads, p->prefix_cap, step);
+        pl.prefix_rows = tile_rows(p->dtype, all / p->n_prefixes);
+        const int64_t tile = pl.prefix_rows, members = std::min<int64_t>(p->n_prefixes, p->batch);  // prefixes with rows, each with a tile that is not full
+        const int64_t tiles = (all + members * (tile - 1)) / tile, parts = parts_for(tiles * p->n_kv_heads, p->prefix_cap, (int)tile);
         pl.prefix_tiles = (int)tiles;
         pl.prefix_parts = (int)parts;
         pl.prefix_items = (p->n_kv_heads * parts + 7) / 8 * 8 * tiles;
     }
     if (pages) {
-        const int64_t tiles = (per + tile - 1) / tile, units = (int64_t)p->batch * p->n_kv_heads;
-        const int64_t parts = parts_for(tiles * units, (int64_t)pages->table_width * pages->page_size, step);
+        const int64_t tiles = (per + pl.tail_rows - 1) / pl.tail_rows, units = (int64_t)p->batch * p->n_kv_heads;
+        const int64_t parts = parts_for(tiles * units, (int64_t)pages->table_width * pages->page_size, pl.tail_rows);
         pl.tail_tiles = (int)tiles;
         pl.tail_parts = (int)parts;
         pl.tail_items = (units * parts + 7) / 8 * 8 * tiles;

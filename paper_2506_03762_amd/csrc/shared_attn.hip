@@ -358,11 +358,28 @@ static hipError_t launch_shared_t(const SharedGeom &g, const SharedPlan &pl, voi
     float2 *part_ms = (float2 *)((char *)ws + pl.off_ms);
     const int64_t items = pl.prefix_items + pl.tail_items;
     if (items > 0) {
-        if constexpr (sizeof(T) == 2)
-            hipLaunchKernelGGL(shared_narrow_kernel<D>, dim3((unsigned)items), dim3(256), 0, st, g, pl, part_o, part_ms);
-        else
-            hipLaunchKernelGGL(shared_f32_kernel<D>, dim3((unsigned)items), dim3(256), 0, st, g, pl, part_o, part_ms);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = [&] {
+            if constexpr (sizeof(T) == 4) {
+                hipLaunchKernelGGL(shared_f32_kernel<D>, dim3((unsigned)items), dim3(256), 0, st, g, pl, part_o, part_ms);
+                return hipGetLastError();
+            } else {
+                auto launch = [&](const SharedPlan &some, int rows) {
+                    if (some.prefix_items + some.tail_items == 0) return hipSuccess;
+                    if (rows > 32) return launch_shared_wide(g, some, rows, part_o, part_ms, st);
+                    hipLaunchKernelGGL(shared_narrow_kernel<D>, dim3((unsigned)(some.prefix_items + some.tail_items)), dim3(256), 0, st, g, some,
+                                       part_o, part_ms);
+                    return hipGetLastError();
+                };
+                if (pl.prefix_rows == pl.tail_rows) return launch(pl, pl.tail_rows);
+                SharedPlan some = pl;
+                some.tail_items = 0;
+                const hipError_t e1 = launch(some, pl.prefix_rows);
+                if (e1 != hipSuccess) return e1;
+                some = pl;
+                some.prefix_items = 0;
+                return launch(some, pl.tail_rows);
+            }
+        }();
         if (e != hipSuccess) return e;
     }
     constexpr int rows = 1024 / D;

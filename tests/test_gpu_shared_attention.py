@@ -122,6 +122,31 @@ def test_logits_that_keep_rising(dtype):
         b.check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_len", [25, 60])
+def test_logits_that_keep_rising_in_large_tiles(d, q_len):
+    """The same with 100 and 240 rows of a prefix and of a tail: references that stay (rises of less than 2^20), that move
+    in some blocks and in all, and weights that would not be numbers without the move."""
+    for slope in (0.003, 0.05, 0.5, 8.0):
+        b = Batch(18, q_heads=4, kv_heads=1, d=d, q_len=q_len, tail=[400], prefix=[1300], page=32)
+        u = torch.randn(d, generator=torch.Generator().manual_seed(1)).to(b.dtype)
+        b.q += u
+        for t in (b.kp, b.kt):
+            t += (torch.arange(t.size(2))[None, None, :, None] * slope * u / 8).to(b.dtype)
+        b.check()
+
+
+@pytest.mark.parametrize("rows,prefix", [(65, 1000), (100, 64), (128, 4097), (129, 500), (200, 4000), (256, 1), (257, 777), (600, 2500)])
+def test_large_tiles(rows, prefix):
+    """Rows around the tiles' sizes, of one prefix and of several, single tokens and chunks."""
+    for d in (64, 128):
+        Batch(rows, q_heads=1, kv_heads=1, d=d, q_len=1, tail=[1 + i % 40 for i in range(rows)], prefix=[prefix], page=8).check()
+        Batch(rows + 1, q_heads=2, kv_heads=2, d=d, q_len=rows, tail=[rows + 100], prefix=[prefix], page=16, holes={(0, 3): -1},
+              layout="bnhd").check()
+    Batch(rows + 2, q_heads=5, kv_heads=1, d=128, q_len=(rows + 9) // 10, tail=[(rows + 9) // 10 + 3] * 6, prefix=[prefix, 300, 0],
+          first=[0, 2, 5, 6], page=1).check()
+
+
 def test_without_lse_and_in_strided_outputs():
     b = Batch(17, q_heads=4, kv_heads=2, d=128, q_len=5, tail=[20, 9], prefix=[200])
     d = b.upload()
