@@ -313,43 +313,73 @@ __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, Shared
 }
 
 // ---- joining a row's parts ----
-// A thread takes four channels of a row.  Parts without a key have a reference of -inf and no output; rows without a prefix have no
-// prefix parts.
-template <class T, int D>
-__global__ __launch_bounds__(256) void shared_join_kernel(SharedGeom g, SharedPlan pl, const float *part_o, const float2 *part_ms) {
-    constexpr int TPR = D / 4;
-    const int per = rows_of_sequence(g), row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
-    if (row >= g.batch * per) return;
-    const int h = blockIdx.y, b = row / per, at = row - b * per, gi = at / g.n, t = at - gi * g.n;
-    if (t >= fresh_of(g, b)) return;
-    int lo = 0, hi = g.n_prefixes;  // prefixes that begin at or before b
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (first_of(g, mid) <= b) lo = mid + 1; else hi = mid;
-    }
-    const bool ahead = lo > 0 && b < first_of(g, lo);
-    const int p0 = ahead ? 0 : pl.prefix_parts, p1 = pl.prefix_parts + pl.tail_parts;
-    float M = -INFINITY, ssum = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = p0; p < p1; ++p) {
-        const int64_t i = partial_index(g, pl, h, p, row);
-        const float2 ms = part_ms[i];
-        if (ms.x == -INFINITY) continue;
-        const f32x4 x = *(const f32x4 *)(part_o + i * D + ch);
-        const float mn = fmaxf(M, ms.x), f0 = exp2f(M - mn), f1 = exp2f(ms.x - mn);
-        ssum = ssum * f0 + f1 * ms.y;
+// A thread takes four channels of a row and every SP-th part, four parts' loads in flight at once (bound by their latency: one
+// after the other, 33 parts took 23 us); the SP threads of a channel meet in LDS.  Parts without a key have a reference of -inf and no
+// output; rows without a prefix have no prefix parts.
+struct JoinState {
+    float m, s;
+    f32x4 o;
+    __device__ __forceinline__ void add(float m1, float s1, const f32x4 &o1) {
+        const float mn = fmaxf(m, m1), ref = mn == -INFINITY ? 0.f : mn, f0 = exp2f(m - ref), f1 = exp2f(m1 - ref);
+        s = s * f0 + s1 * f1;
+        if (m1 != -INFINITY) {  // (else o1 may be anything)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = o[c] * f0 + f1 * x[c];
-        M = mn;
+            for (int c = 0; c < 4; ++c) o[c] = o[c] * f0 + o1[c] * f1;
+        }
+        m = mn;
     }
-    const float inv = ssum == 0.f ? 0.f : 1.f / ssum;
+};
+template <class T, int D, int SP>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedGeom g, SharedPlan pl, const float *part_o, const float2 *part_ms) {
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * SP), U = 4;
+    const int per = rows_of_sequence(g), ch = threadIdx.x % TPR * 4, sp = threadIdx.x / TPR % SP;
+    const int row = blockIdx.x * ROWS + threadIdx.x / (TPR * SP);
+    const int h = blockIdx.y, b = min(row / per, g.batch - 1), at = row - b * per, gi = at / g.n, t = at - gi * g.n;
+    const bool live = row < g.batch * per && t < fresh_of(g, b);
+    JoinState x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+    if (live) {
+        int lo = 0, hi = g.n_prefixes;  // prefixes that begin at or before b
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (first_of(g, mid) <= b) lo = mid + 1; else hi = mid;
+        }
+        const bool ahead = lo > 0 && b < first_of(g, lo);
+        const int p0 = ahead ? 0 : pl.prefix_parts, p1 = pl.prefix_parts + pl.tail_parts;
+        const int64_t step = partial_index(g, pl, 0, 1, 0);
+        for (int p = p0 + sp; p < p1; p += U * SP) {
+            const int64_t i = partial_index(g, pl, h, p, row);
+            float2 ms[U];
+            f32x4 o[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {  // (past the last part: the first of these again)
+                const int64_t j = p + u * SP < p1 ? i + u * SP * step : i;
+                ms[u] = part_ms[j];
+                o[u] = *(const f32x4 *)(part_o + j * D + ch);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * SP < p1) x.add(ms[u].x, ms[u].y, o[u]);
+        }
+    }
+    if constexpr (SP > 1) {
+        __shared__ f32x4 s_o[256];
+        __shared__ float2 s_ms[256];
+        s_o[threadIdx.x] = x.o;
+        s_ms[threadIdx.x] = make_float2(x.m, x.s);
+        __syncthreads();
+        if (sp) return;
+#pragma unroll
+        for (int u = 1; u < SP; ++u) x.add(s_ms[threadIdx.x + u * TPR].x, s_ms[threadIdx.x + u * TPR].y, s_o[threadIdx.x + u * TPR]);
+    }
+    if (!live) return;
+    const float inv = x.s == 0.f ? 0.f : 1.f / x.s;
     T *out = (T *)g.out + b * g.os[0] + (h * g.G + gi) * g.os[1] + t * g.os[2] + ch;
     if constexpr (sizeof(T) == 2) {
-        *(uint2 *)out = uint2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+        *(uint2 *)out = uint2{pack_bf16(x.o[0] * inv, x.o[1] * inv), pack_bf16(x.o[2] * inv, x.o[3] * inv)};
     } else {
-        *(f32x4 *)out = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        *(f32x4 *)out = f32x4{x.o[0] * inv, x.o[1] * inv, x.o[2] * inv, x.o[3] * inv};
     }
-    if (g.lse && ch == 0) g.lse[((int64_t)b * g.Hq + h * g.G + gi) * g.n + t] = ssum == 0.f ? -INFINITY : (M + log2f(ssum)) * kLn2;
+    if (g.lse && ch == 0) g.lse[((int64_t)b * g.Hq + h * g.G + gi) * g.n + t] = x.s == 0.f ? -INFINITY : (x.m + log2f(x.s)) * kLn2;
 }
 
 template <class T, int D>
@@ -382,9 +412,13 @@ static hipError_t launch_shared_t(const SharedGeom &g, const SharedPlan &pl, voi
         }();
         if (e != hipSuccess) return e;
     }
-    constexpr int rows = 1024 / D;
-    const int total = g.batch * g.G * g.n;
-    hipLaunchKernelGGL((shared_join_kernel<T, D>), dim3((unsigned)((total + rows - 1) / rows), g.Hkv), dim3(256), 0, st, g, pl, part_o, part_ms);
+    const int64_t total = (int64_t)g.batch * g.G * g.n;
+    auto join = [&](auto kernel, int rows) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((total + rows - 1) / rows), g.Hkv), dim3(256), 0, st, g, pl, part_o, part_ms);
+    };
+    // (up to four parts are in flight at once anyway)
+    if (pl.prefix_parts + pl.tail_parts <= 4) join(shared_join_kernel<T, D, 1>, 256 / (D / 4));
+    else join(shared_join_kernel<T, D, 8>, 256 / (D / 4 * 8));
     return hipGetLastError();
 }
 

@@ -88,6 +88,12 @@ __device__ __forceinline__ bool shared_item(const SharedGeom &g, const SharedPla
     const int steps = (keys + step - 1) / step;
     it.begin = (int)((int64_t)part * steps / parts) * step;
     it.end = min(keys, (int)((int64_t)(part + 1) * steps / parts) * step);
+    // (the same in all lanes, which the compiler cannot know of what was loaded)
+    it.which = uniform(it.which);
+    it.row0 = uniform(it.row0);
+    it.row1 = uniform(it.row1);
+    it.begin = uniform(it.begin);
+    it.end = uniform(it.end);
     return true;
 }
 

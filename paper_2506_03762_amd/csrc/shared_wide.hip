@@ -28,8 +28,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr float kWideMost = 0x1p20f;
 
 // x *= f where x lives in accumulator registers: written in assembly so that the compiler keeps it there on both ways past this
-// rarely taken branch (else it copies all outputs to vector registers and back twice per 32 keys).  The waits are those
-// between a product and a read of its result, and between a write and a product.
+// rarely taken branch (else it copies all outputs to vector registers and back in every block).  The waits are those between a
+// product and a read of its result, and between a write and a product.
 template <int CB>
 __device__ __forceinline__ void scale_outputs(f32x16 (&O)[CB], float f) {
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -48,9 +48,9 @@ __device__ __forceinline__ void scale_outputs(f32x16 (&O)[CB], float f) {
 
 template <int D, int RW>
 struct WideShared {
-    static constexpr int WAVES = 4, KW = WAVES / RW, KEYS = 64, NB = KEYS / 32 / KW;  // blocks of a wave per stage
-    static constexpr int CPR = D / 8, RPI = 64 / CPR, NI = KEYS / RPI / WAVES;        // load instructions per wave for a stage's keys (values)
-    static constexpr int kStages = 4;
+    static constexpr int WAVES = 4, KW = WAVES / RW, KEYS = 32 * KW;
+    static constexpr int CPR = D / 8, RPI = 64 / CPR, NI = KEYS / RPI / WAVES;  // load instructions per wave for a stage's keys (values)
+    static constexpr int kStages = D == 64 || KW == 1 ? 8 : 4;
     static constexpr int kbytes = KeyRows<D>::bytes(KEYS), vbytes = KEYS * D * 2;
     static constexpr int off_values = kStages * kbytes, off_pages = off_values + kStages * vbytes;
     static constexpr int kEntries = 2048;  // page numbers kept in LDS (a longer range reads the others from memory)
@@ -88,49 +88,48 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
     };
 
     // ---- stages ----
-    // Instruction i = wave + 4 j of a stage covers RPI rows, lane -> row lane / CPR, place lane % CPR; the 16-byte chunks of a row are
-    // permuted on the way.  The loads are assembly and the waits for them by hand (value_rows.h).
+    // Load j of a stage covers RPI rows of group wave + 4 j, lane -> row lane / CPR, place lane % CPR; the 16-byte chunks of a
+    // row are permuted on the way.  The loads are assembly and the waits for them by hand (value_rows.h).
     const uint32_t lds0 = uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem);
     const int lr = lane / A::CPR, lc = lane % A::CPR;
     const int kchunk = lc ^ KeyRows<D>::swizzle(lr), vchunk = lc ^ value_chunk_swizzle<D>(lr);
-    const uint32_t k_off = (uint32_t)(lr * keys.ks * 2) + kchunk * 16, v_off = (uint32_t)(lr * keys.vs * 2) + vchunk * 16;
-    const bool near = it.prefix && keys.ks * 2 * A::RPI < ((int64_t)1 << 31) && keys.vs * 2 * A::RPI < ((int64_t)1 << 31);
-    auto request = [&](int stage) {  // (past the last one: zeros)
-        const int kb = it.begin + stage * A::KEYS, st = stage % S;
-        const uint32_t kdst = lds0 + st * A::kbytes + wave * KeyRows<D>::group, vdst = lds0 + A::off_values + st * A::vbytes + wave * 1024;
-        if (near && kb + A::KEYS <= it.end) {
-            const __bf16 *k0 = keys.k + (int64_t)(kb + wave * A::RPI) * keys.ks, *v0 = keys.v + (int64_t)(kb + wave * A::RPI) * keys.vs;
+    const int stages = (it.end - it.begin + A::KEYS - 1) / A::KEYS;
+    const int whole = it.prefix ? (it.end - it.begin) / A::KEYS : 0;  // stages whose rows follow from those of the one before
+    const int64_t k_step = A::KEYS * keys.ks, v_step = A::KEYS * keys.vs;
+    const __bf16 *k_at[NI], *v_at[NI];  // what the lane loads of the stage to come
+    auto locate = [&](int stage) {      // (stages have to be located one by one; past the last one: zeros)
+        if (stage > 0 && stage < whole) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j)
-                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                             :
-                             : "v"(k_off), "s"(k0 + (int64_t)(A::WAVES * A::RPI * j) * keys.ks), "s"(kdst + j * A::WAVES * KeyRows<D>::group)
-                             : "memory");
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                             :
-                             : "v"(v_off), "s"(v0 + (int64_t)(A::WAVES * A::RPI * j) * keys.vs), "s"(vdst + j * A::WAVES * 1024)
-                             : "memory");
+            for (int j = 0; j < NI; ++j) k_at[j] += k_step, v_at[j] += v_step;
             return;
         }
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int key = kb + (wave + A::WAVES * j) * A::RPI + lr;
+            const int key = it.begin + stage * A::KEYS + (wave + A::WAVES * j) * A::RPI + lr;
             const auto row = keys.at(key, !it.prefix && key < it.end ? entry(key) : 0);
-            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                         :
-                         : "v"(row.k + kchunk * 8), "s"(kdst + j * A::WAVES * KeyRows<D>::group)
-                         : "memory");
-            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                         :
-                         : "v"(row.v + vchunk * 8), "s"(vdst + j * A::WAVES * 1024)
-                         : "memory");
+            k_at[j] = row.k + kchunk * 8;
+            v_at[j] = row.v + vchunk * 8;
         }
     };
-    const int stages = (it.end - it.begin + A::KEYS - 1) / A::KEYS;
+    auto load_to_lds = [&](const __bf16 *from, int to) {
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(uniform((int)lds0 + to)) : "memory");
+    };
+    auto request_keys = [&](int place, int j) { load_to_lds(k_at[j], place * A::kbytes + (wave + A::WAVES * j) * KeyRows<D>::group); };
+    auto request_values = [&](int place, int j) {
+        load_to_lds(v_at[j], A::off_values + place * A::vbytes + (wave + A::WAVES * j) * 1024);
+    };
+    auto request = [&](int stage) {
+        locate(stage);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) request_keys(stage % S, j);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) request_values(stage % S, j);
+    };
 
-    // ---- the wave's rows ----
+    // ---- the wave's rows, which travel with the first stages ----
+    // (loops that are not unrolled, here and where it does not count: straight code that runs once is fetched from memory line by line)
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) request(i);
     bf16x8 qf[2][KS];
     int limit[2], limit_min;
     uint32_t live[2];
@@ -152,11 +151,11 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
         limit_min = uniform(least);
     }
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) request(i);
-#pragma unroll
     for (int q = 0; q < 2; ++q)  // (no load of the compiler's is waited for in the loop)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[q][ks]));
+#pragma unroll 1
+    for (int i = 2; i < S - 1; ++i) request(i);
 
     const float c_out = pl.c_out;
     f32x16 O[2][CB], acc[2];
@@ -179,12 +178,10 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
         for (int v = 0; v < 16; ++v) am[v & 1] = fmaxf(am[v & 1], x[v]);
         return combine_lane_xor<32>(fmaxf(am[0], am[1]), OpMax{}) * c_out;
     };
-    // Block b of a wave: keys [key_of(b), + 32), block kw + KW (b % NB) of stage b / NB.
-    auto key_of = [&](int b) { return it.begin + b / A::NB * A::KEYS + (kw + KW * (b % A::NB)) * 32; };
-    auto key_rows = [&](int b) { return smem + (b / A::NB) % S * A::kbytes + (kw + KW * (b % A::NB)) * KeyRows<D>::bytes(32); };
-    auto value_rows = [&](int b) {
-        return (const __bf16 *)(smem + A::off_values + (b / A::NB) % S * A::vbytes) + (kw + KW * (b % A::NB)) * 32 * D;
-    };
+    // block b of the wave, in stage b: keys [key_of(b), + 32)
+    auto key_of = [&](int b) { return it.begin + b * A::KEYS + kw * 32; };
+    auto key_rows = [&](int b) { return smem + b % S * A::kbytes + kw * KeyRows<D>::bytes(32); };
+    auto value_rows = [&](int b) { return (const __bf16 *)(smem + A::off_values + b % S * A::vbytes) + kw * 32 * D; };
     // Logits of block b that row block q does not see become -inf; a row that has seen no key so far takes its reference, the
     // largest logit of its first keys.
     auto finish = [&](int q, int b) {
@@ -206,11 +203,19 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
             if (m[q] == -INFINITY) m[q] = top;
         }
     };
-    // A phase: exponentials of row block q, products of the other one; in phase 0 the fragments are replaced by those of the next
-    // keys and of these keys' values.  The vector work lies between the products in the order in which it is written (without
-    // the empty assembly the compiler moves it behind them).
-    auto phase = [&](auto which, const char *next_keys, const __bf16 *these_values) {
+    // A phase of block b: exponentials of row block q, products of the other one; in phase 0 the fragments are replaced by those of
+    // the next keys and of these keys' values.  The vector work lies between the products in the order in which it is written (without
+    // the empty assembly the compiler moves it behind them), and so do half of a later stage's loads: issued together they
+    // hold the waves up, 16 cycles per load and wave.
+    auto phase = [&](auto which, int b) {
         constexpr int q = decltype(which)::value, o = 1 - q;
+        const char *next_keys = key_rows(b + 1);
+        const __bf16 *these_values = value_rows(b);
+        auto load = [&](int slot) {
+            if (slot % (SLOTS / NI) != 0) return;
+            if (q == 0) request_keys((b + S - 1) % S, slot / (SLOTS / NI));
+            else request_values((b + S - 1) % S, slot / (SLOTS / NI));
+        };
         float sum[2], pr[16];
         const float mref = m[q] == -INFINITY ? 0.f : m[q];
         auto pack = [&](int e) {  // e, e + 1
@@ -237,6 +242,7 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
             acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[o][ks], ks ? acc[o] : zero, 0, 0, 0);
             if (q == 0) kf[ks] = key_fragment(next_keys, place, ks);
             weigh(ks);
+            load(ks);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -244,11 +250,11 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
             O[o][i % CB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[o][i / CB], O[o][i % CB], 0, 0, 0);
             if (q == 0) vf[i] = value_fragment<D>(these_values, 0, i / CB, i % CB, lane);
             weigh(KS + i);
+            load(KS + i);
             __builtin_amdgcn_sched_barrier(0);
         }
         pack(14);
-        const float all = sum[0] + (sum[1] + pr[15]);
-        const float before = s[q];
+        const float all = sum[0] + (sum[1] + pr[15]), before = s[q];
         s[q] += all;
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(all > kWideMost) != 0, 0)) {
             // far above the reference: a new one, the largest logit, and these weights again
@@ -275,29 +281,35 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    const int blocks = stages * A::NB;
     advance();
-    if (mine) {
+    if (!mine) {  // (no rows: only its share of the loads)
+        for (int st = 0; st < stages; ++st) {
+            advance();
+            request(st + S - 1);
+        }
+    } else {
         const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks] = key_fragment(key_rows(0), place, ks);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[0][ks], ks ? acc[0] : zero, 0, 0, 0);
         finish(0, 0);
-    }
-    for (int st = 0; st < stages; ++st) {
-#pragma unroll
-        for (int x = 0; x < A::NB; ++x) {
-            const int b = st * A::NB + x;
-            if (x == A::NB - 1) {  // the next keys lie in the next stage
+        using P0 = std::integral_constant<int, 0>;
+        using P1 = std::integral_constant<int, 1>;
+        for (int st = 0; st < stages;) {
+            advance();
+            locate(st + S - 1);
+            phase(P0{}, st);
+            finish(1, st);
+            phase(P1{}, st);
+            if (++st < stages) finish(0, st);
+            // where the keys and the next ones are whole, with a reference in every row, there are only the phases
+            if (__builtin_amdgcn_ballot_w64(m[0] == -INFINITY || m[1] == -INFINITY) != 0) continue;
+            for (; st + 2 <= whole; ++st) {
                 advance();
-                request(st + S - 1);
-            }
-            if (mine) {
-                phase(std::integral_constant<int, 0>{}, key_rows(b + 1), value_rows(b));
-                finish(1, b);
-                phase(std::integral_constant<int, 1>{}, nullptr, nullptr);
-                if (b + 1 < blocks) finish(0, b + 1);
+                locate(st + S - 1);
+                phase(P0{}, st);
+                phase(P1{}, st);
             }
         }
     }
