@@ -16,6 +16,59 @@ namespace aha {
 constexpr float kRefSlack = 8.f;  // log2 units that a reference may lie below the running maximum
 constexpr float kLn2 = 0.69314718055994531f;
 
+// ---- the waves' results of an item of 32 rows -> the workspace ----
+// Lane: row lane % 32, accumulator element v of channel block cb: channel 32 cb + 8 (v / 4) + 4 (lane / 32) + v % 4.  Every wave scales
+// its output to the largest reference, half of the channels at a time meet in LDS, and a thread adds four channels of the
+// waves' rows (with a channel at a time and its weights formed there, 4 us of an item's 10; so 1).
+template <int D>
+struct WaveMerge {
+    static constexpr int WAVES = 4, HC = D / 2, LDO = HC + 4;  // channels at a time, floats of a row
+    static constexpr size_t o_bytes = (size_t)WAVES * 32 * LDO * 4, bytes = o_bytes + (size_t)WAVES * 32 * 8;
+};
+template <int D>
+__device__ __forceinline__ void merge_waves(const SharedGeom &g, const SharedPlan &pl, const SharedItem &it, bool live_row, f32x16 (&O)[D / 32],
+                                            float m, float s, char *smem, int lane, int wave, float *part_o, float2 *part_ms) {
+    using A = WaveMerge<D>;
+    constexpr int CB = D / 32, CPR = A::HC / 4;
+    const int tid = wave * 64 + lane, col = lane & 31, hf = lane >> 5, rows = it.row1 - it.row0;
+    float2 *sMS = (float2 *)(smem + A::o_bytes);
+    __syncthreads();  // what the LDS held is done with
+    const float sc = combine_lane_xor<32>(s, OpSum{});
+    if (lane < 32) sMS[wave * 32 + lane] = make_float2(m, sc);
+    const uint32_t live = (uint32_t)__builtin_amdgcn_ballot_w64(live_row);
+    __syncthreads();
+    float M = -INFINITY, all = 0.f;
+#pragma unroll
+    for (int w = 0; w < A::WAVES; ++w) M = fmaxf(M, sMS[w * 32 + col].x);
+    const float mref = M == -INFINITY ? 0.f : M, f = fast_exp2(m - mref);
+#pragma unroll
+    for (int w = 0; w < A::WAVES; ++w) all = fmaf(fast_exp2(sMS[w * 32 + col].x - mref), sMS[w * 32 + col].y, all);
+    if (tid < 32 && live_row) part_ms[partial_index(g, pl, it.h, it.part, it.row0 + col)] = make_float2(M, all);
+#pragma unroll
+    for (int hc = 0; hc < 2; ++hc) {
+        float *sO = (float *)smem + (wave * 32 + col) * A::LDO + 4 * hf;
+        if (hc) __syncthreads();
+        if (live_row) {
+#pragma unroll
+            for (int cb = 0; cb < CB / 2; ++cb)
+#pragma unroll
+                for (int v = 0; v < 16; v += 4) {
+                    const f32x16 &x = O[hc * (CB / 2) + cb];
+                    *(f32x4 *)(sO + cb * 32 + 2 * v) = f32x4{x[v] * f, x[v + 1] * f, x[v + 2] * f, x[v + 3] * f};
+                }
+        }
+        __syncthreads();
+        for (int i = tid; i < rows * CPR; i += 256) {
+            const int q = i / CPR, ch = i % CPR * 4;
+            if (!((live >> q) & 1)) continue;
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < A::WAVES; ++w) o += *(const f32x4 *)((const float *)smem + (w * 32 + q) * A::LDO + ch);
+            *(f32x4 *)(part_o + partial_index(g, pl, it.h, it.part, it.row0 + q) * D + hc * A::HC + ch) = o;
+        }
+    }
+}
+
 // ---- bf16, up to 32 rows ----
 // Four waves take blocks of 32 keys in turn, each with all rows: a stream of keys and values, bound by memory.  Per block and
 // wave: S^T = K Q^T and O^T += V^T P^T by v_mfma_f32_32x32x16_bf16, keys (channels) on M, rows on N, so that the accumulator elements of a
@@ -23,11 +76,9 @@ constexpr float kLn2 = 0.69314718055994531f;
 template <int D>
 struct NarrowAttn {
     static constexpr int WAVES = 4, STEP = 32 * WAVES, CPR = D / 8, RPI = 64 / CPR, NI = 32 / RPI;
-    static constexpr int HC = D / 2, LDO = HC + 1;  // channels per pass of the waves' merge, floats of a row there
     static constexpr size_t v_bytes = 32 * D * 2;   // a block's value rows
-    static constexpr size_t o_bytes = (size_t)WAVES * 32 * LDO * 4, merge_bytes = o_bytes + (size_t)WAVES * 32 * 8;
     static constexpr size_t stage_bytes = 2 * WAVES * v_bytes;
-    static constexpr size_t bytes = stage_bytes > merge_bytes ? stage_bytes : merge_bytes;
+    static constexpr size_t bytes = stage_bytes > WaveMerge<D>::bytes ? stage_bytes : WaveMerge<D>::bytes;
 };
 template <int D>
 __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
@@ -147,43 +198,7 @@ __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, Sha
     }
     wait_loads<0>();
 
-    // ---- the waves' partials meet in LDS, half of the channels at a time ----
-    __syncthreads();
-    float2 *sMS = (float2 *)(smem + A::o_bytes);
-    const float sc = combine_lane_xor<32>(s, OpSum{});
-    if (lane < 32) sMS[wave * 32 + lane] = make_float2(m, sc);
-    const int rows = it.row1 - it.row0;
-    const uint32_t live = (uint32_t)__builtin_amdgcn_ballot_w64(row.live);
-#pragma unroll
-    for (int hc = 0; hc < 2; ++hc) {
-        float *sO = (float *)smem + wave * 32 * A::LDO;
-        if (hc) __syncthreads();
-#pragma unroll
-        for (int cb = 0; cb < CB / 2; ++cb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (col < rows) sO[col * A::LDO + cb * 32 + 8 * (v >> 2) + 4 * hf + (v & 3)] = O[hc * (CB / 2) + cb][v];
-        __syncthreads();
-        for (int i = tid; i < rows * A::HC; i += 256) {
-            const int q = i / A::HC, ch = i % A::HC;
-            if (!((live >> q) & 1)) continue;
-            float M = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < A::WAVES; ++w) M = fmaxf(M, sMS[w * 32 + q].x);
-            const float mref = M == -INFINITY ? 0.f : M;
-            float o = 0.f, ssum = 0.f;
-#pragma unroll
-            for (int w = 0; w < A::WAVES; ++w) {
-                const float2 ms = sMS[w * 32 + q];
-                const float f = fast_exp2(ms.x - mref);
-                o = fmaf(f, ((const float *)smem)[(w * 32 + q) * A::LDO + ch], o);
-                ssum = fmaf(f, ms.y, ssum);
-            }
-            const int64_t p = partial_index(g, pl, it.h, it.part, it.row0 + q);
-            part_o[p * D + hc * A::HC + ch] = o;
-            if (hc == 0 && ch == 0) part_ms[p] = make_float2(M, ssum);
-        }
-    }
+    merge_waves<D>(g, pl, it, row.live, O, m, s, smem, lane, wave, part_o, part_ms);
 }
 
 // ---- fp32 ----
@@ -192,9 +207,8 @@ __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, Sha
 // contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.
 template <int D>
 struct F32Attn {
-    static constexpr int WAVES = 4, STEP = 32 * WAVES, HC = D / 2, LDO = HC + 1, LDQ = f32_ld(D);
-    static constexpr size_t o_bytes = (size_t)WAVES * 32 * LDO * 4, q_bytes = (size_t)32 * LDQ * 4;
-    static constexpr size_t bytes = (o_bytes > q_bytes ? o_bytes : q_bytes) + (size_t)WAVES * 32 * 8;
+    static constexpr int WAVES = 4, STEP = 32 * WAVES, LDQ = f32_ld(D);
+    static constexpr size_t q_bytes = (size_t)32 * LDQ * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
 };
 template <int D>
 __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
@@ -274,42 +288,7 @@ __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, Shared
             for (int cb = 0; cb < CB; ++cb) O[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[cb * 32], acc[v], O[cb], 0, 0, 0);
         }
     }
-    __syncthreads();  // the query rows are done with
-    float2 *sMS = (float2 *)(smem + A::bytes - (size_t)A::WAVES * 32 * 8);
-    const float sc = combine_lane_xor<32>(s, OpSum{});
-    if (lane < 32) sMS[wave * 32 + lane] = make_float2(m, sc);
-    const int rows = it.row1 - it.row0;
-    const uint32_t live = (uint32_t)__builtin_amdgcn_ballot_w64(row.live);
-#pragma unroll
-    for (int hc = 0; hc < 2; ++hc) {
-        float *sO = (float *)smem + wave * 32 * A::LDO;
-        if (hc) __syncthreads();
-#pragma unroll
-        for (int cb = 0; cb < CB / 2; ++cb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (col < rows) sO[col * A::LDO + cb * 32 + 8 * (v >> 2) + 4 * hf + (v & 3)] = O[hc * (CB / 2) + cb][v];
-        __syncthreads();
-        for (int i = tid; i < rows * A::HC; i += 256) {
-            const int q = i / A::HC, ch = i % A::HC;
-            if (!((live >> q) & 1)) continue;
-            float M = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < A::WAVES; ++w) M = fmaxf(M, sMS[w * 32 + q].x);
-            const float mref = M == -INFINITY ? 0.f : M;
-            float o = 0.f, ssum = 0.f;
-#pragma unroll
-            for (int w = 0; w < A::WAVES; ++w) {
-                const float2 ms = sMS[w * 32 + q];
-                const float f = fast_exp2(ms.x - mref);
-                o = fmaf(f, ((const float *)smem)[(w * 32 + q) * A::LDO + ch], o);
-                ssum = fmaf(f, ms.y, ssum);
-            }
-            const int64_t p = partial_index(g, pl, it.h, it.part, it.row0 + q);
-            part_o[p * D + hc * A::HC + ch] = o;
-            if (hc == 0 && ch == 0) part_ms[p] = make_float2(M, ssum);
-        }
-    }
+    merge_waves<D>(g, pl, it, row.live, O, m, s, smem, lane, wave, part_o, part_ms);
 }
 
 // ---- joining a row's parts ----

@@ -77,10 +77,16 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
     const SharedKeys<__bf16> keys(g, it);
     int32_t *pages = (int32_t *)(smem + A::off_pages);
     const int entry0 = it.begin >> keys.shift;
+    bool holes = false;  // in the item's pages (or so many pages that it is not known)
     if (!it.prefix) {
-        const int n = min(A::kEntries, ((it.end - 1) >> keys.shift) - entry0 + 1);
-        for (int i = tid; i < n; i += 256) pages[i] = keys.table[entry0 + i];
-        __syncthreads();
+        const int all = ((it.end - 1) >> keys.shift) - entry0 + 1, n = min(A::kEntries, all);
+        bool bad = n < all;
+        for (int i = tid; i < n; i += 256) {
+            const int page = keys.table[entry0 + i];
+            pages[i] = page;
+            bad |= page < 0 || page >= keys.pages;
+        }
+        holes = __syncthreads_or(bad);
     }
     auto entry = [&](int key) {  // the page of a tail's key (before `end`)
         const int i = (key >> keys.shift) - entry0;
@@ -186,12 +192,12 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
     // largest logit of its first keys.
     auto finish = [&](int q, int b) {
         const int kb = key_of(b);
-        if (kb + 32 > it.end || kb + 31 > limit_min || !it.prefix) {
-            uint32_t there = 0xffffffffu;
-            if (!it.prefix) {
-                const int key = kb + col, page = key < it.end ? entry(key) : -1;
-                there = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0 && page < keys.pages);
-            }
+        uint32_t there = 0xffffffffu;
+        if (!it.prefix) {
+            const int key = kb + col, page = key < it.end ? entry(key) : -1;
+            there = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0 && page < keys.pages);
+        }
+        if (kb + 32 > it.end || kb + 31 > limit_min || there != 0xffffffffu) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int at = 8 * (v >> 2) + 4 * hf + (v & 3);
@@ -294,6 +300,7 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[0][ks], ks ? acc[0] : zero, 0, 0, 0);
         finish(0, 0);
+        const int plain = holes ? 0 : (int)max((int64_t)0, min((int64_t)it.end, (int64_t)limit_min + 1) - it.begin) / A::KEYS;
         using P0 = std::integral_constant<int, 0>;
         using P1 = std::integral_constant<int, 1>;
         for (int st = 0; st < stages;) {
@@ -303,9 +310,9 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
             finish(1, st);
             phase(P1{}, st);
             if (++st < stages) finish(0, st);
-            // where the keys and the next ones are whole, with a reference in every row, there are only the phases
+            // where all rows see all keys, and the next ones, and have a reference, there are only the phases
             if (__builtin_amdgcn_ballot_w64(m[0] == -INFINITY || m[1] == -INFINITY) != 0) continue;
-            for (; st + 2 <= whole; ++st) {
+            for (; st + 2 <= plain; ++st) {
                 advance();
                 locate(st + S - 1);
                 phase(P0{}, st);
