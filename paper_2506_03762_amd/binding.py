@@ -365,13 +365,18 @@ class _Described:
         self.tensors = tuple(t + (t[0] in _DENSE,) for t in tensors)
 
 
-def _check_tensors(tensors, given):
-    device = torch._C._cuda_getDevice()
+def _pointers(tensors, given):
+    """The given tensors' addresses, once they are what the description says."""
+    device, out = torch._C._cuda_getDevice(), []
     for (name, dtype, n, dense), t in zip(tensors, given):
-        if t is not None and (t.dtype is not dtype or t.numel() != n or t.get_device() != device or
-                              (dense and not t.is_contiguous())):
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not dtype or t.numel() != n or t.get_device() != device or (dense and not t.is_contiguous()):
             raise ValueError("%s: not a%s tensor of %d elements of %s on the current device" % (
                 name, " contiguous" if dense else "", n, dtype))
+        out.append(t.data_ptr())
+    return out
 
 
 class Rotary(_Described):
@@ -399,7 +404,8 @@ class Rotary(_Described):
         self = cls(p, (p.batch, p.n_kv_heads, p.head_dim, dt), ("q", dt, nq), ("k", dt, nk),
                    ("inv_freq", torch.float32, pairs), ("pair_axis", torch.int32, pairs),
                    ("positions", torch.int32, p.n_axes * p.batch * p.tokens), ("q_out", dt, nq), ("k_out", dt, nk))
-        self.appended = self.tensors[:6] + (("v", dt, nk, False),)
+        q, k, freq, axis, pos, q_out = self.tensors[:6]
+        self.appended = (q, k, ("v", dt, nk, False), freq, axis, pos, q_out)
         return self
 
 
@@ -441,9 +447,10 @@ class SharedAttention(_Described):
             n, p.n_prefixes, p.prefix_cap = k_prefix.numel(), k_prefix.size(0), k_prefix.size(2)
             p.k_stride, p.v_stride = _view("k_prefix", k_prefix, q), _view("v_prefix", v_prefix, q)
         return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), ("q", q.dtype, q.numel()),
-                   ("k_prefix", q.dtype, n), ("v_prefix", q.dtype, n), ("prefix_len", torch.int32, p.n_prefixes), ("prefix_first", torch.int32, p.n_prefixes + 1),
-                   ("out", q.dtype, q.numel()), ("lse", torch.float32, q.numel() // p.head_dim),
-                   ("new_len", torch.int32, p.batch))
+                   ("k_prefix", q.dtype, n), ("v_prefix", q.dtype, n),
+                   ("prefix_len", torch.int32, p.n_prefixes), ("prefix_first", torch.int32, p.n_prefixes + 1),
+                   ("new_len", torch.int32, p.batch), ("out", q.dtype, q.numel()),
+                   ("lse", torch.float32, q.numel() // p.head_dim))
 
 
 def rotary_tables(rot_dim: int, base: float = 10000.0, sections=None, device="cuda"):
@@ -461,20 +468,17 @@ def rotary_tables(rot_dim: int, base: float = 10000.0, sections=None, device="cu
 
 def aha_rotate(p: Rotary, q, k, inv_freq, pair_axis, positions, q_out, k_out):
     """q_out, k_out <- the rows of q, k turned by positions [axes, b, n] (int32)."""
-    _check_tensors(p.tensors, (q, k, inv_freq, pair_axis, positions, q_out, k_out))
-    _check((_lib or load()).aha_rotate(
-        p, _ptr(q), _ptr(k), _ptr(inv_freq), _ptr(pair_axis), _ptr(positions), _ptr(q_out), _ptr(k_out), _stream()))
+    at = _pointers(p.tensors, (q, k, inv_freq, pair_axis, positions, q_out, k_out))
+    _check((_lib or load()).aha_rotate(p, *at, _stream()))
 
 
 def aha_append_paged(p: Rotary, cache: Pages, q, k, v, inv_freq, pair_axis, positions, page_table, tail_len, new_len,
                      q_out, k_pages, v_pages):
     """The new tokens' keys (turned) and values into their places of the pools; q_out <- q turned."""
-    _check_tensors(p.appended, (q, k, inv_freq, pair_axis, positions, q_out, v))
-    _check_tensors(cache.tensors, (k_pages, v_pages, page_table, tail_len, new_len))
     _check_same(p, cache)
-    _check((_lib or load()).aha_append_paged(
-        p, cache, _ptr(q), _ptr(k), _ptr(v), _ptr(inv_freq), _ptr(pair_axis), _ptr(positions), _ptr(page_table),
-        _ptr(tail_len), _ptr(new_len), _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _stream()))
+    at = _pointers(p.appended + cache.tensors, (q, k, v, inv_freq, pair_axis, positions, q_out, k_pages, v_pages,
+                                                page_table, tail_len, new_len))
+    _check((_lib or load()).aha_append_paged(p, cache, *at[:6], *at[9:], *at[6:9], _stream()))
 
 
 def _check_same(p, cache: Pages):
@@ -497,10 +501,10 @@ def aha_shared_attention(p: SharedAttention, cache: Optional[Pages], q, k_prefix
                          k_pages, v_pages, page_table, tail_len, new_len, out, lse, workspace):
     """out [b, Hq, n, d], lse [b, Hq, n] (fp32 or None) <- attention of the new tokens over their shared prefix
     and their own tail."""
-    _check_tensors(p.tensors, (q, k_prefix, v_prefix, prefix_len, prefix_first, out, lse, new_len))
+    expected, given = p.tensors, (q, k_prefix, v_prefix, prefix_len, prefix_first, new_len, out, lse)
     if cache is not None:
-        _check_tensors(cache.tensors, (k_pages, v_pages, page_table, tail_len))
         _check_same(p, cache)
-    _check((_lib or load()).aha_shared_attention(
-        p, cache, _ptr(q), _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_len), _ptr(prefix_first), _ptr(k_pages),
-        _ptr(v_pages), _ptr(page_table), _ptr(tail_len), _ptr(new_len), _ptr(out), _ptr(lse), *_ws(workspace), _stream()))
+        expected, given = expected + cache.tensors[:4], given + (k_pages, v_pages, page_table, tail_len)
+    at = _pointers(expected, given)
+    tails = at[8:] if cache is not None else [_ptr(t) for t in (k_pages, v_pages, page_table, tail_len)]
+    _check((_lib or load()).aha_shared_attention(p, cache, *at[:5], *tails, *at[5:8], *_ws(workspace), _stream()))

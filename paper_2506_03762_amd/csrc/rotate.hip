@@ -92,16 +92,10 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotaryGeom g, int per) {
     const RowChunks<T> ch(c, g.rot, NEIGHBOURS);
     int64_t k_at = 0, v_at = 0;  // APPEND: the token's row in the pools, without the head
     bool placed = true;
+    int fresh = g.n;
     if constexpr (APPEND) {
-        const int fresh = g.pages.new_len ? min(g.pages.new_len[b], g.n) : g.n;
+        if (g.pages.new_len) fresh = min(g.pages.new_len[b], g.n);
         if (t >= fresh) return;  // padding
-        const int64_t slot = (int64_t)g.pages.tail_len[b] - fresh + t, entry = slot >> g.pages.page_shift;
-        placed = slot >= 0 && entry < g.pages.table_width;
-        const int page = placed ? g.pages.table[(int64_t)b * g.pages.table_width + entry] : -1;
-        placed = page >= 0 && page < g.pages.n_pages;
-        const int row = (int)slot & ((1 << g.pages.page_shift) - 1);
-        k_at = page * g.pages.ks[0] + row * g.pages.ks[2];
-        v_at = page * g.pages.vs[0] + row * g.pages.vs[2];
     }
     auto source = [&](int h) {
         const T *p = h < g.Hq            ? (const T *)g.q + b * g.qs[0] + h * g.qs[1] + t * g.qs[2]
@@ -126,6 +120,15 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotaryGeom g, int per) {
         }
     };
     request(h0);
+    if constexpr (APPEND) {  // (looked up while the rows travel)
+        const int64_t slot = (int64_t)g.pages.tail_len[b] - fresh + t, entry = slot >> g.pages.page_shift;
+        placed = slot >= 0 && entry < g.pages.table_width;
+        const int page = placed ? g.pages.table[(int64_t)b * g.pages.table_width + entry] : -1;
+        placed = page >= 0 && page < g.pages.n_pages;
+        const int row = (int)slot & ((1 << g.pages.page_shift) - 1);
+        k_at = page * g.pages.ks[0] + row * g.pages.ks[2];
+        v_at = page * g.pages.vs[0] + row * g.pages.vs[2];
+    }
     float cs[CE], sn[CE];
 #pragma unroll
     for (int i = 0; i < CE; ++i) cs[i] = 1.f, sn[i] = 0.f;
@@ -163,9 +166,13 @@ template <class T, int D, bool NEIGHBOURS, bool APPEND>
 static hipError_t launch_rotate_t(const RotaryGeom &g, hipStream_t st) {
     constexpr int tokens = 256 * 2 * RowChunks<T>::CE / D;
     const int64_t tiles = ((int64_t)g.batch * g.n + tokens - 1) / tokens;
-    const int heads = g.Hq + (APPEND ? 2 : 1) * g.Hkv, most = (heads + kHeadsAhead - 1) / kHeadsAhead;
-    // heads are dealt over workgroups, each of which forms the angles again, until 2048 workgroups have work (eight per CU)
-    const int64_t split = std::min<int64_t>(std::max<int64_t>(1, (2048 + tiles - 1) / tiles), most);
+    const int heads = g.Hq + (APPEND ? 2 : 1) * g.Hkv;
+    // Heads are dealt over workgroups, each of which forms the angles again.  Few heads to a workgroup where a head's tokens lie
+    // together (32768 tokens, 32 + 8 heads: 145 us with 2048 workgroups, 134 with 4096; not where pages are written, 8 x 2048 ragged
+    // tokens 52 and 57), many where a token's heads do (3 x 5003 tokens, 12 + 4 heads, 36 us with 2048, 30 with 512).
+    const bool token_major = g.Hq > 1 ? g.qs[1] < g.qs[2] : g.Hkv > 1 && g.ks[1] < g.ks[2];
+    const int64_t target = token_major ? 512 : APPEND ? 2048 : 4096;
+    const int64_t split = std::min<int64_t>(std::max<int64_t>(1, (target + tiles - 1) / tiles), heads);
     const int per = (int)((heads + split - 1) / split);
     hipLaunchKernelGGL((rotate_kernel<T, D, NEIGHBOURS, APPEND>), dim3((unsigned)tiles, (heads + per - 1) / per), dim3(256), 0, st, g, per);
     return hipGetLastError();
