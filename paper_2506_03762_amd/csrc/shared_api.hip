@@ -126,10 +126,10 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
 
 // Rows of a tile for about `rows` rows that see the same keys.
 static int tile_rows(int dtype, int64_t rows) { return dtype != AHA_BF16 || rows <= 64 ? 32 : rows <= 128 ? 128 : 256; }
-// Parts of an item's keys: as many as fill the chip (two workgroups per CU, large tiles one) with `tiles` in each, of two steps at
-// least (large tiles four).
+// Parts of an item's keys: as many as fill the chip (two workgroups per CU, large tiles one) with `tiles` in each, large tiles of four steps at
+// least.
 static int64_t parts_for(int64_t tiles, int64_t keys, int rows) {
-    const int64_t step = rows > 32 ? 64 : 128, steps = (keys + step - 1) / step, resident = rows > 32 ? 256 : 512, least = rows > 32 ? 4 : 2;
+    const int64_t step = rows > 32 ? 64 : 128, steps = (keys + step - 1) / step, resident = rows > 32 ? 256 : 512, least = rows > 32 ? 4 : 1;
     return std::max<int64_t>(1, std::min<int64_t>({(resident + tiles - 1) / tiles, (steps + least - 1) / least, 64}));
 }
 static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {

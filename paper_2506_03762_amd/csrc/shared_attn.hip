@@ -205,6 +205,25 @@ __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, Sha
 // The same on v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it): a lane's chunks of a key row and a query
 // row as in f32_tile.h; the second product takes the probabilities from the accumulators one element at a time, a
 // contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.
+// The dots of 32 keys and 32 rows in four chains of D / 4 products: eight, as in f32_tile.h, leave no room beside the outputs (d = 128, 8
+// sequences of one prefix of 2048 keys 26.3 us, so 21.6; 2 x 64 rows x 4 heads, 4096 keys 57.4, 49.5; d = 64 37.2, 29.0).
+template <int D>
+__device__ __forceinline__ f32x16 dots_f32(const f32x4 (&a)[D / 8], const float *sq) {
+    f32x16 acc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[c][v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+        const f32x4 q = *(const f32x4 *)(sq + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i][e], q[e], acc[e], 0, 0, 0);
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[0][v] = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
+    return acc[0];
+}
 template <int D>
 struct F32Attn {
     static constexpr int WAVES = 4, STEP = 32 * WAVES, LDQ = f32_ld(D);
@@ -251,7 +270,8 @@ __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, Shared
         f32x4 a[D / 8];
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) a[i] = *(const f32x4 *)(here.k + 4 * hf + 8 * i);
-        f32x16 acc = f32_block_dots<D>(a, sq);
+        f32x16 acc = dots_f32<D>(a, sq);
+        __builtin_amdgcn_sched_barrier(0);  // (value rows requested in front of the products take the registers of the chains)
         if (there != 0xffffffffu || kb + 31 > limit_min) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {

@@ -53,12 +53,13 @@ __device__ __forceinline__ int prefix_of_tile(const SharedGeom &g, int rows, int
     return -1;
 }
 
-// Work item of workgroup `id`: prefixes' items first.  Items of the same keys get numbers that are congruent modulo the XCDs, whose
+// Work item of workgroup `id`: the tails' items first, whose lengths differ most (64 sequences of four prefixes of 4096 tokens 63.3 us
+// with the prefixes' first, so 59.5).  Items of the same keys get numbers that are congruent modulo the XCDs, whose
 // workgroups share an L2.  `rows`: of a tile; `step`: keys that ranges are multiples of.  false: nothing to do.
 __device__ __forceinline__ bool shared_item(const SharedGeom &g, const SharedPlan &pl, int id, int rows, int step, int lane,
                                             SharedItem &it) {
-    it.prefix = id < pl.prefix_items;
-    if (!it.prefix) id -= (int)pl.prefix_items;
+    it.prefix = id >= pl.tail_items;
+    if (it.prefix) id -= (int)pl.tail_items;
     const int tiles = it.prefix ? pl.prefix_tiles : pl.tail_tiles, parts = it.prefix ? pl.prefix_parts : pl.tail_parts;
     const int t = id / kXcds, unit = t / tiles * kXcds + id % kXcds, per = rows_of_sequence(g);
     int tile = t % tiles, keys, part = unit % parts;

@@ -121,7 +121,7 @@ class Batch:
         """out, tolerance, lse, tolerance of all rows (NaN where nothing is written), in 64 bits.
 
         Tolerances.  A logit is a sum of d products in fp32: off by `delta` = 20 half steps of the scaled sum of
-        the products' sizes (chains of up to d / 8 additions, joined), which a weight is off by relatively, twice with
+        the products' sizes (chains of up to d / 4 additions, whose roundings are a random walk, joined), which a weight is off by relatively, twice with
         the normaliser.  Sums over the keys: 4 sqrt(keys) + 16 half steps (a random walk).  bf16: weights go
         into the second product rounded to bf16, independent errors of 2^-8 at most, whose sum has a standard deviation
         of 2^-8 / sqrt(3) |(p_j v_j)|; six of them.  And the output's own half step."""
