@@ -27,15 +27,16 @@ __device__ __forceinline__ int fresh_of(const SharedGeom &g, int b) {
     return g.pages.new_len ? min(max(g.pages.new_len[b], 0), g.n) : g.n;
 }
 
-// The prefix whose tile number `tile` is (tiles are counted prefix by prefix), and the number among its own; -1: there are
-// fewer.  64 prefixes at a time, one per lane; all lanes of a wave call it and get the same.
-__device__ __forceinline__ int prefix_of_tile(const SharedGeom &g, int rows, int &tile, int lane) {
+// The prefix whose tile number `tile` is (tiles are counted prefix by prefix): its first and last sequence and its length; `tile` becomes the
+// number among its own.  -1: there are fewer tiles.  64 prefixes at a time, one per lane, so that all that a work item has to
+// know comes with one round of loads; all lanes of a wave call it and get the same.
+__device__ __forceinline__ int prefix_of_tile(const SharedGeom &g, int rows, int lane, int &tile, int &first, int &end, int &len) {
     const int per = rows_of_sequence(g);
     for (int base = 0; base < g.n_prefixes; base += 64) {
         const int i = base + lane;
-        int tiles = 0;
-        if (i < g.n_prefixes) tiles = max(0, first_of(g, i + 1) - first_of(g, i)) * per;
-        tiles = (tiles + rows - 1) / rows;
+        int lo = 0, hi = 0, n = 0;
+        if (i < g.n_prefixes) lo = first_of(g, i), hi = first_of(g, i + 1), n = min(max(g.prefix_len[i], 0), g.prefix_cap);
+        const int tiles = (max(0, hi - lo) * per + rows - 1) / rows;
         int sum = tiles;  // over the lanes up to this one
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) {
@@ -46,6 +47,9 @@ __device__ __forceinline__ int prefix_of_tile(const SharedGeom &g, int rows, int
         if (beyond) {
             const int at = __builtin_ctzll(beyond);
             tile -= __shfl(sum - tiles, at);
+            first = __shfl(lo, at);
+            end = __shfl(hi, at);
+            len = __shfl(n, at);
             return base + at;
         }
         tile -= __shfl(sum, 63);
@@ -66,12 +70,11 @@ __device__ __forceinline__ bool shared_item(const SharedGeom &g, const SharedPla
     it.h = unit / parts % g.Hkv;
     if (it.prefix) {
         if (unit >= g.Hkv * parts) return false;
-        it.which = uniform(prefix_of_tile(g, rows, tile, lane));
-        tile = uniform(tile);
+        int first, end;
+        it.which = uniform(prefix_of_tile(g, rows, lane, tile, first, end, keys));
         if (it.which < 0) return false;
-        keys = min(max(g.prefix_len[it.which], 0), g.prefix_cap);
-        it.row0 = first_of(g, it.which) * per + tile * rows;
-        it.row1 = min(it.row0 + rows, first_of(g, it.which + 1) * per);
+        it.row0 = first * per + tile * rows;
+        it.row1 = min(it.row0 + rows, end * per);
         it.part = part;
     } else {
         if (unit >= g.batch * g.Hkv * parts) return false;
