@@ -167,11 +167,12 @@ static hipError_t launch_rotate_t(const RotaryGeom &g, hipStream_t st) {
     constexpr int tokens = 256 * 2 * RowChunks<T>::CE / D;
     const int64_t tiles = ((int64_t)g.batch * g.n + tokens - 1) / tokens;
     const int heads = g.Hq + (APPEND ? 2 : 1) * g.Hkv;
-    // Heads are dealt over workgroups, each of which forms the angles again.  Few heads to a workgroup where a head's tokens lie
-    // together (32768 tokens, 32 + 8 heads: 145 us with 2048 workgroups, 134 with 4096; not where pages are written, 8 x 2048 ragged
-    // tokens 52 and 57), many where a token's heads do (3 x 5003 tokens, 12 + 4 heads, 36 us with 2048, 30 with 512).
-    const bool token_major = g.Hq > 1 ? g.qs[1] < g.qs[2] : g.Hkv > 1 && g.ks[1] < g.ks[2];
-    const int64_t target = token_major ? 512 : APPEND ? 2048 : 4096;
+    // Heads are dealt over workgroups, each of which forms the angles again, until 384 workgroups have work (us with 256, 384, 512, 1024, 4096
+    // of them: 8 x 821 tokens, 32 + 8 heads, turned 31.5, 31.6, 33.4, 35.8, 46.2; appended 37.3, 37.4, 39.8, 42.6, 50.6; 8 x 200 turned
+    // 11.1, 11.2, 10.7, 13.1, 18.1); four to a tile for long prompts whose heads' tokens lie together (32768 tokens 145.5 with one,
+    // 135.6).
+    const bool head_major = g.Hq > 1 ? g.qs[1] > g.qs[2] : g.ks[1] > g.ks[2];
+    const int64_t target = !APPEND && head_major && tiles >= 1024 ? 4 * tiles : 384;
     const int64_t split = std::min<int64_t>(std::max<int64_t>(1, (target + tiles - 1) / tiles), heads);
     const int per = (int)((heads + split - 1) / split);
     hipLaunchKernelGGL((rotate_kernel<T, D, NEIGHBOURS, APPEND>), dim3((unsigned)tiles, (heads + per - 1) / per), dim3(256), 0, st, g, per);
