@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libaha.so: argument marshalling only.
+"""Thin ctypes binding of libaha.so: argument marshalling.
 
 Every step of the eviction path runs in the HIP kernels behind the C ABI of
 ``include/aha.h``; the functions here take torch tensors (device memory owned

@@ -124,7 +124,9 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
     return check_stride("v", p->v_stride, p->dtype, p->head_dim);
 }
 
-// Rows of a tile for about `rows` rows that see the same keys.
+// Rows of a tile for about `rows` rows that see the same keys.  us of a call with tiles of 32 and of 128 rows: 64 rows of 8 heads, 16384 keys
+// 27.3, 36.2; 4 x 64 rows, 4096 keys, d = 64 34.8, 42.4; 128 rows of 8 heads 40.8, 44.1 for 16384 keys, 69.5, 58.1 for 32768; 128 rows of 32
+// heads 124.8, 89.4; with tiles of 32 and of 256: 192 rows of 8 heads 60.2, 50.2.
 static int tile_rows(int dtype, int64_t rows) { return dtype != AHA_BF16 || rows <= 64 ? 32 : rows <= 128 ? 128 : 256; }
 // Parts of an item's keys: as many as fill the chip (two workgroups per CU, large tiles one) with `tiles` in each, large tiles of four steps at
 // least.
