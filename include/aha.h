@@ -397,7 +397,7 @@ enum { AHA_PAIR_HALVES = 0, AHA_PAIR_NEIGHBOURS = 1 };
  *             the inputs.
  */
 typedef struct aha_rotary {
-    int32_t batch;        /* batch * tokens <= 2^30 */
+    int32_t batch;        /* batch * tokens <= 2^27 */
     int32_t tokens;       /* rows per sequence and head */
     int32_t n_q_heads;    /* any two numbers >= 1 */
     int32_t n_kv_heads;
@@ -490,7 +490,7 @@ int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void
  */
 typedef struct aha_shared {
     int32_t batch;        /* batch * n_kv_heads <= 65535 */
-    int32_t q_len;        /* rows per sequence, >= 1; n_q_heads / n_kv_heads * q_len * batch <= 2^24 */
+    int32_t q_len;        /* rows per sequence, >= 1; n_q_heads / n_kv_heads * q_len * batch <= 2^22 */
     int32_t n_q_heads;
     int32_t n_kv_heads;
     int32_t head_dim;     /* 64 or 128 */

@@ -397,6 +397,8 @@ class Rotary(_Described):
         for name, t in (("q", q), ("k", k), ("v", v), ("q_out", q_out), ("k_out", k_out)):
             if t is not None:
                 setattr(p, name + "_stride", _view(name, t, given))
+        if any(t is not None and (x is None or t.shape != x.shape) for t, x in ((q_out, q), (k_out, k), (v, k))):
+            raise ValueError("q_out, or k_out or v, has another shape than q, or k")
         if q is not None and k is not None and (q.size(0), q.size(2)) != (k.size(0), k.size(2)):
             raise ValueError("q and k have other batches or tokens")
         rows, dt, pairs = p.batch * p.tokens * p.head_dim, given.dtype, p.rot_dim // 2

@@ -31,7 +31,8 @@ static int32_t check_rotary(const aha_rotary *p) {
     if (!p) return fail(AHA_ERR_INVALID_ARG, "params is null");
     const int32_t rc = check_heads(p->batch, p->tokens, "tokens", p->n_q_heads, p->n_kv_heads, p->head_dim, p->dtype);
     if (rc) return rc;
-    if ((int64_t)p->batch * p->tokens > 1 << 30) return fail(AHA_ERR_UNSUPPORTED, "batch * tokens beyond 2^30");
+    // (up to 16 threads a row: a launch has fewer than 2^32)
+    if ((int64_t)p->batch * p->tokens > 1 << 27) return fail(AHA_ERR_UNSUPPORTED, "batch * tokens beyond 2^27");
     if ((int64_t)p->n_q_heads + 2 * (int64_t)p->n_kv_heads > 65535)
         return fail(AHA_ERR_UNSUPPORTED, "n_q_heads + 2 n_kv_heads exceeds 65535");
     if (p->rot_dim < 0 || p->rot_dim > p->head_dim || p->rot_dim % 16 != 0)
@@ -106,8 +107,8 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
     if (p->n_q_heads % p->n_kv_heads != 0)
         return fail(AHA_ERR_INVALID_ARG, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
     const int64_t rows = (int64_t)(p->n_q_heads / p->n_kv_heads) * p->q_len;  // (each factor below 2^31)
-    if ((int64_t)p->batch * p->n_kv_heads > 65535 || rows > 1 << 24 || rows * p->batch > 1 << 24)
-        return fail(AHA_ERR_UNSUPPORTED, "batch * n_kv_heads exceeds 65535 or group * q_len * batch 2^24");
+    if ((int64_t)p->batch * p->n_kv_heads > 65535 || rows > 1 << 22 || rows * p->batch > 1 << 22)
+        return fail(AHA_ERR_UNSUPPORTED, "batch * n_kv_heads exceeds 65535 or group * q_len * batch 2^22");
     if (p->n_prefixes < 0 || (p->n_prefixes > 0 && p->prefix_cap < 1))
         return fail(AHA_ERR_INVALID_ARG, "n_prefixes must be >= 0, prefix_cap >= 1");
     if (p->n_prefixes > 65535 || (p->n_prefixes > 0 && p->prefix_cap > 1 << 30))
@@ -161,8 +162,10 @@ static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {
     return pl;
 }
 
+// (workgroups of 256 threads: a launch has fewer than 2^32)
 static int32_t check_items(const SharedPlan &pl) {
-    if (pl.prefix_items + pl.tail_items > 1 << 30) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
+    if (pl.prefix_items + pl.tail_items > 1 << 23)
+        return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
     return AHA_OK;
 }
 

@@ -81,6 +81,25 @@ def test_members_in_many_groups():
           first=first, page=16).check()
 
 
+def test_more_prefixes_than_lanes():
+    rng = np.random.default_rng(4)
+    batch, n = 190, 150
+    first = np.sort(rng.integers(0, batch + 1, size=n + 1)).tolist()
+    Batch(19, q_heads=2, kv_heads=1, d=64, q_len=1, tail=rng.integers(1, 20, batch).tolist(), prefix=rng.integers(0, 60, n).tolist(),
+          first=first, page=16).check()
+
+
+@BOTH
+def test_nothing_to_attend_to(dtype):
+    """Neither prefixes nor tails: zeros, and -inf."""
+    Batch(20, q_heads=4, kv_heads=2, d=64, q_len=3, tail=[0, 0], new=[3, 1], dtype=dtype, tails=False).check()
+
+
+def test_more_pages_than_a_large_tile_keeps():
+    """256 (sequence, KV head) problems, so that one item has a tail's 2500 pages of a token each; some are holes."""
+    Batch(21, q_heads=128, kv_heads=128, d=64, q_len=70, tail=[2500, 2300], page=1, holes={(0, 5): -1, (0, 2200): -1, (1, 2299): -1}).check()
+
+
 def random_batch(seed):
     rng = np.random.default_rng(seed)
     log = lambda lo, hi: int(round(np.exp(rng.uniform(np.log(lo), np.log(hi)))))

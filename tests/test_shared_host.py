@@ -71,6 +71,7 @@ BAD, NOT_BUILT, WS = B.AHA_ERR_INVALID_ARG, B.AHA_ERR_UNSUPPORTED, B.AHA_ERR_WOR
     (dict(head_dim=96), NOT_BUILT), (dict(dtype=2), BAD), (dict(rot_dim=136), BAD), (dict(rot_dim=24), BAD),
     (dict(rot_dim=-16), BAD), (dict(pairing=2), BAD), (dict(n_axes=0), BAD), (dict(n_axes=5), BAD), (dict(transpose=2), BAD),
     (dict(batch=1 << 20, tokens=1 << 11), NOT_BUILT), (dict(n_q_heads=65535), NOT_BUILT),
+    (dict(batch=1, tokens=(1 << 27) + 1), NOT_BUILT),                    # more threads than a launch may have
     (dict(q_stride=three(102400, 12800, 64)), BAD), (dict(q_stride=three(102400, 12801, 128)), BAD),
     (dict(q_stride=three(-8, 12800, 128)), BAD), (dict(q_out_stride=three(0, 12800, 128)), BAD),
     (dict(q_out_stride=three(102400, 0, 128)), BAD),
@@ -111,6 +112,7 @@ def test_append_arguments_are_refused():
     (dict(batch=0), BAD), (dict(q_len=0), BAD), (dict(n_q_heads=7), BAD), (dict(head_dim=256), NOT_BUILT), (dict(dtype=-1), BAD),
     (dict(n_prefixes=-1), BAD), (dict(prefix_cap=0), BAD), (dict(prefix_cap=(1 << 30) + 1), NOT_BUILT), (dict(n_prefixes=70000), NOT_BUILT),
     (dict(scale=-0.1), BAD), (dict(scale=float("nan")), BAD), (dict(scale=float("inf")), BAD), (dict(reserved=3), BAD),
+    (dict(q_len=1 << 19, batch=1, n_q_heads=65535 * 8, n_kv_heads=65535), NOT_BUILT),     # likewise
     (dict(batch=40000), NOT_BUILT), (dict(q_len=1 << 23), NOT_BUILT), (dict(q_len=1 << 30, n_q_heads=1 << 20), NOT_BUILT),
 ])
 def test_shared_descriptions_are_refused(kw, code):
@@ -162,6 +164,10 @@ def test_descriptions_of_tensors():
         B.Rotary.of(None, None)
     with pytest.raises(ValueError):
         B.Rotary.of(q, k[:1], q)
+    with pytest.raises(ValueError):
+        B.Rotary.of(q, k, q.reshape(2, 3, 8, 64))
+    with pytest.raises(ValueError):
+        B.Rotary.of(None, k, q)
     with pytest.raises(ValueError):
         B.Rotary.of(q.transpose(2, 3), None, q)
     with pytest.raises(ValueError):
