@@ -162,7 +162,7 @@ class Batch:
     # ---- the framework's side ----
     def upload(self):
         from paper_2506_03762_amd import binding as B
-        dev = lambda t: torch.empty_strided(t.size(), t.stride(), dtype=t.dtype, device="cuda").copy_(t)
+        dev = lambda t: (t.cuda() if 0 in t.stride() else torch.empty_strided(t.size(), t.stride(), dtype=t.dtype, device="cuda").copy_(t))
         i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
         d = dict(q=dev(self.q), tail=i32(self.tail), new=None if self.new is None else i32(self.new))
         d["out"] = torch.full_like(d["q"], float("nan"))

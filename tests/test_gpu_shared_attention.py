@@ -100,6 +100,47 @@ def test_more_pages_than_a_large_tile_keeps():
     Batch(21, q_heads=128, kv_heads=128, d=64, q_len=70, tail=[2500, 2300], page=1, holes={(0, 5): -1, (0, 2200): -1, (1, 2299): -1}).check()
 
 
+@BOTH
+@pytest.mark.parametrize("q_len", [3, 90])
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, q_len):
+    """Keys of one sequence's newest token, and values and keys of another one's old ones, that are NaN or infinite: the rows
+    that do not see them get the same bits as without them, the others no numbers."""
+    b = Batch(22, q_heads=4, kv_heads=2, d=64, q_len=q_len, tail=[q_len + 5, q_len + 30, q_len + 70], prefix=[200], page=16, dtype=dtype)
+    d = b.upload()
+    b.run(d)
+    b.check(d)
+    clean = d["out"].clone(), d["lse"].clone()
+    for fill in (float("nan"), float("inf"), -float("inf")):
+        kt, vt = b.kt.clone(), b.vt.clone()
+        _, page, row = b.slots(0)[-1]
+        kt[page, :, row] = fill                     # the newest token of sequence 0: seen by its last row alone
+        _, page, row = b.slots(2)[3]
+        vt[page, :, row] = fill                     # an old one of sequence 2: seen by all its rows
+        d["kt"].copy_(kt)
+        d["vt"].copy_(vt)
+        b.run(d)
+        torch.cuda.synchronize()
+        for got, was in zip((d["out"], d["lse"]), clean):
+            assert torch.equal(got[1], was[1]) and torch.equal(got[0, :, :-1], was[0, :, :-1])
+        assert torch.equal(d["lse"][2], clean[1][2])
+        assert not torch.isfinite(d["out"][2].float()).any()
+        assert not torch.equal(d["lse"][0, :, -1], clean[1][0, :, -1])
+
+
+def test_heads_that_share_a_prefix():
+    """A prefix whose KV heads are one (a stride of 0), and queries that all heads share."""
+    b = Batch(23, q_heads=4, kv_heads=2, d=128, q_len=2, tail=[9, 30], prefix=[300], page=16)
+    b.q = b.q[:, :1].expand(-1, 4, -1, -1)
+    b.kp, b.vp = (t[:, :1].expand(-1, 2, -1, -1) for t in (b.kp, b.vp))
+    d = b.upload()
+    for x, t in (("q", b.q), ("kp", b.kp), ("vp", b.vp)):
+        d[x] = t[:, :1].contiguous().cuda().expand_as(t)
+    from paper_2506_03762_amd import binding as B
+    d["p"] = B.SharedAttention.of(d["q"], d["out"], d["kp"], d["vp"], b.scale)
+    b.run(d)
+    b.check(d)
+
+
 def random_batch(seed):
     rng = np.random.default_rng(seed)
     log = lambda lo, hi: int(round(np.exp(rng.uniform(np.log(lo), np.log(hi)))))
