@@ -337,13 +337,15 @@ def default_fixed_scale(head_dim: int) -> float:
 
 
 # ---- a prompt that several sequences continue: rotation, the paged cache, attention behind shared prefixes ----
-# A description is made once (its C struct is built then, and the sizes that its tensors have) and serves every call
-# with tensors of these shapes and strides.  Per call their element types, sizes and devices are compared, not their
-# strides: 0.3 us a tensor.
+# A description is made once (its C struct is built then) and serves every call with tensors of these shapes and strides.
+# The kernels address rows by the described strides alone, so each call compares shapes, strides, element types and devices:
+# another layout of as many elements would be read, or written, outside its memory.  (Sizes alone cost 0.2 us of host time less
+# for each tensor of rows: 64 single tokens appended 8.2 us a call, so 9.4.)
 
 _CODES = {torch.float32: AHA_F32, torch.bfloat16: AHA_BF16}
-# what has no strides of its own
-_DENSE = ("inv_freq", "pair_axis", "positions", "page_table", "tail_len", "new_len", "prefix_len", "prefix_first", "lse")
+# what has no strides of its own: element types
+_DENSE = dict.fromkeys(("pair_axis", "positions", "page_table", "tail_len", "new_len", "prefix_len", "prefix_first"), torch.int32)
+_DENSE.update(inv_freq=torch.float32, lse=torch.float32)
 
 
 def _view(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
@@ -357,24 +359,37 @@ def _view(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
 
 class _Described:
     """The C struct of a description, its rows' (batch, KV heads, head size, dtype), and of its tensors, in the order
-    in which a call takes them, names, element types and numbers of elements."""
+    in which a call takes them: names, element types, numbers of elements (dense ones) or shapes and strides."""
 
-    def __init__(self, struct, rows, *tensors):
+    def __init__(self, struct, rows, dtype, *tensors):
+        """tensors: name and number of elements, or name and the tensor that is described (None: not given)."""
         self._as_parameter_ = ctypes.byref(struct)
         self.struct, self.rows = struct, rows
-        self.tensors = tuple(t + (t[0] in _DENSE,) for t in tensors)
+        self.tensors = tuple(
+            (name, _DENSE[name], t, None, None) if name in _DENSE else
+            (name, dtype, None, (), ()) if t is None else (name, dtype, None, t.shape, t.stride())
+            for name, t in tensors)
+
+
+def _same_places(t, shape, stride):
+    """Whether t's elements lie as described: axes of one element have any stride, or are left out."""
+    return [x for x in zip(t.shape, t.stride()) if x[0] != 1] == [x for x in zip(shape, stride) if x[0] != 1]
 
 
 def _pointers(tensors, given):
     """The given tensors' addresses, once they are what the description says."""
     device, out = torch._C._cuda_getDevice(), []
-    for (name, dtype, n, dense), t in zip(tensors, given):
+    for (name, dtype, n, shape, stride), t in zip(tensors, given):
         if t is None:
             out.append(None)
             continue
-        if t.dtype is not dtype or t.numel() != n or t.get_device() != device or (dense and not t.is_contiguous()):
-            raise ValueError("%s: not a%s tensor of %d elements of %s on the current device" % (
-                name, " contiguous" if dense else "", n, dtype))
+        if shape is None:
+            if t.dtype is not dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous():
+                raise ValueError("%s: not a contiguous tensor of %d elements of %s on the current device" % (name, n, dtype))
+        elif t.dtype is not dtype or t.get_device() != device or (
+                (t.stride() != stride or t.shape != shape) and not (shape and _same_places(t, shape, stride))):
+            raise ValueError("%s: not a tensor of %s on the current device with the described shape %s and strides %s" % (
+                name, dtype, tuple(shape), stride) if shape else "%s is given, but not described" % name)
         out.append(t.data_ptr())
     return out
 
@@ -401,13 +416,12 @@ class Rotary(_Described):
             raise ValueError("q_out, or k_out or v, has another shape than q, or k")
         if q is not None and k is not None and (q.size(0), q.size(2)) != (k.size(0), k.size(2)):
             raise ValueError("q and k have other batches or tokens")
-        rows, dt, pairs = p.batch * p.tokens * p.head_dim, given.dtype, p.rot_dim // 2
-        nq, nk = rows * p.n_q_heads, rows * p.n_kv_heads
-        self = cls(p, (p.batch, p.n_kv_heads, p.head_dim, dt), ("q", dt, nq), ("k", dt, nk),
-                   ("inv_freq", torch.float32, pairs), ("pair_axis", torch.int32, pairs),
-                   ("positions", torch.int32, p.n_axes * p.batch * p.tokens), ("q_out", dt, nq), ("k_out", dt, nk))
-        q, k, freq, axis, pos, q_out = self.tensors[:6]
-        self.appended = (q, k, ("v", dt, nk, False), freq, axis, pos, q_out)
+        self = cls(p, (p.batch, p.n_kv_heads, p.head_dim, given.dtype), given.dtype, ("q", q), ("k", k),
+                   ("inv_freq", p.rot_dim // 2), ("pair_axis", p.rot_dim // 2),
+                   ("positions", p.n_axes * p.batch * p.tokens), ("q_out", q_out), ("k_out", k_out), ("v", v))
+        q, k, freq, axis, pos, q_out, k_out, v = self.tensors
+        self.tensors = (q, k, freq, axis, pos, q_out, k_out)
+        self.appended = (q, k, v, freq, axis, pos, q_out)
         return self
 
 
@@ -421,11 +435,10 @@ class Pages(_Described):
                       k_stride=_view("k_pages", k_pages), v_stride=_view("v_pages", v_pages, k_pages))
         if k_pages.shape != v_pages.shape:
             raise ValueError("the pools have different shapes")
-        n, batch = k_pages.numel(), page_table.size(0)
-        return cls(p, (batch, k_pages.size(1), k_pages.size(3), k_pages.dtype),
-                   ("k_pages", k_pages.dtype, n), ("v_pages", k_pages.dtype, n),
-                   ("page_table", torch.int32, page_table.numel()), ("tail_len", torch.int32, batch),
-                   ("new_len", torch.int32, batch))
+        batch = page_table.size(0)
+        return cls(p, (batch, k_pages.size(1), k_pages.size(3), k_pages.dtype), k_pages.dtype,
+                   ("k_pages", k_pages), ("v_pages", v_pages), ("page_table", page_table.numel()), ("tail_len", batch),
+                   ("new_len", batch))
 
 
 class SharedAttention(_Described):
@@ -444,15 +457,13 @@ class SharedAttention(_Described):
                        q_stride=_view("q", q), out_stride=_view("out", out, q))
         if q.shape != out.shape or (k_prefix is not None and k_prefix.shape != v_prefix.shape):
             raise ValueError("q and out, or the prefixes' keys and values, have different shapes")
-        n = 0
         if k_prefix is not None:
-            n, p.n_prefixes, p.prefix_cap = k_prefix.numel(), k_prefix.size(0), k_prefix.size(2)
+            p.n_prefixes, p.prefix_cap = k_prefix.size(0), k_prefix.size(2)
             p.k_stride, p.v_stride = _view("k_prefix", k_prefix, q), _view("v_prefix", v_prefix, q)
-        return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), ("q", q.dtype, q.numel()),
-                   ("k_prefix", q.dtype, n), ("v_prefix", q.dtype, n),
-                   ("prefix_len", torch.int32, p.n_prefixes), ("prefix_first", torch.int32, p.n_prefixes + 1),
-                   ("new_len", torch.int32, p.batch), ("out", q.dtype, q.numel()),
-                   ("lse", torch.float32, q.numel() // p.head_dim))
+        return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), q.dtype, ("q", q),
+                   ("k_prefix", k_prefix), ("v_prefix", None if k_prefix is None else v_prefix),
+                   ("prefix_len", p.n_prefixes), ("prefix_first", p.n_prefixes + 1),
+                   ("new_len", p.batch), ("out", out), ("lse", q.numel() // p.head_dim))
 
 
 def rotary_tables(rot_dim: int, base: float = 10000.0, sections=None, device="cuda"):
