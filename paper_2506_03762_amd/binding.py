@@ -519,5 +519,7 @@ def aha_shared_attention(p: SharedAttention, cache: Optional[Pages], q, k_prefix
         _check_same(p, cache)
         expected, given = expected + cache.tensors[:4], given + (k_pages, v_pages, page_table, tail_len)
     at = _pointers(expected, given)
+    if workspace is not None and (workspace.get_device() != torch._C._cuda_getDevice() or not workspace.is_contiguous()):
+        raise ValueError("workspace: not a contiguous tensor on the current device")
     tails = at[8:] if cache is not None else [_ptr(t) for t in (k_pages, v_pages, page_table, tail_len)]
     _check((_lib or load()).aha_shared_attention(p, cache, *at[:5], *tails, *at[5:8], *_ws(workspace), _stream()))

@@ -131,3 +131,20 @@ def test_what_is_not_described_is_refused(calls):
     with pytest.raises(ValueError):
         B.aha_shared_attention(s, None, k, pool, pool, None, None, None, None, None, None, None, k, None, None)
     assert calls == ["aha_rotate"]
+
+
+def test_workspace(calls):
+    """One of another device, or whose elements share their memory, would be written outside its memory."""
+    q = rows(2, 2, 3, 64)
+    s = B.SharedAttention.of(q, q, n_kv_heads=2)
+    def attend(workspace):
+        B.aha_shared_attention(s, None, q, None, None, None, None, None, None, None, None, None, q, None, workspace)
+    class OfAnotherDevice(torch.Tensor):
+        def get_device(self):
+            return 0
+    attend(torch.zeros(256, dtype=torch.uint8))
+    attend(None)
+    for workspace in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(256, dtype=torch.uint8).as_subclass(OfAnotherDevice)):
+        with pytest.raises(ValueError):
+            attend(workspace)
+    assert calls == ["aha_shared_attention"] * 2
