@@ -4,8 +4,9 @@
 // element read and written, so the bytes bound it.  What keeps the angles off that path: a thread owns the same
 // sixteen-byte chunks of a token's row in all heads, forms the sines and cosines of its eight pairs (fp32: four) once, while the
 // first heads' rows travel, and then goes through the heads.  Positions may be far (2^31) and the frequency 1: the
-// angle is formed in turns in double, its whole turns taken away there, and only the rest, at most half a
-// turn, becomes an fp32 number (off by 2^-26 of a turn at most, 1e-7 of the result).
+// angle is formed in turns from a frequency in two doubles (with one it is off by up to 2^-52 of its turns, 7e-8 of a turn
+// at 2^31), its whole turns are taken away there, and only the rest, at most half a turn, becomes an fp32
+// number (off by 2^-26 of a turn at most, 1e-7 of the result).
 //
 // 32768 tokens of 32 + 8 heads, d = 128: 671 MB in 134 us, 5.0 TB/s (a copy reaches 4.8); 3 x 5003 tokens of 12 + 4 heads 23 us for the kernel, 29 a
 // call.  64 single tokens: 6 us, the round trips of tail length, page and store.
@@ -15,6 +16,8 @@
 #include "aha_host.h"
 
 namespace aha {
+
+constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;  // 1 / (2 pi), and what is left of it
 
 // A row of d channels as D / CE chunks of 16 bytes, two of them per thread: of the rotated channels those whose elements
 // make pairs, of the others two neighbours.
@@ -141,8 +144,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotaryGeom g, int per) {
             const int f = c * CE + i;
             const int axis = g.pair_axis ? min(max(g.pair_axis[f], 0), g.n_axes - 1) : 0;
             const int pos = g.positions[(int64_t)axis * g.batch * g.n + token];
-            double turns = (double)pos * ((double)g.inv_freq[f] * 0.15915494309189533577);
-            turns -= rint(turns);
+            const double w = (double)g.inv_freq[f], w1 = w * kTurn, w2 = fma(w, kTurn, -w1) + w * kTurnRest;
+            const double turns = fma((double)pos, w2, fma((double)pos, w1, -rint((double)pos * w1)));
             sincospif(2.f * (float)turns, &sn[i], &cs[i]);
             if (g.transpose) sn[i] = -sn[i];
         }
