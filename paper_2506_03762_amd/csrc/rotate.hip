@@ -6,7 +6,7 @@
 // first heads' rows travel, and then goes through the heads.  Positions may be far (2^31) and the frequency 1: the
 // angle is formed in turns from a frequency in two doubles (with one it is off by up to 2^-52 of its turns, 7e-8 of a turn
 // at 2^31), its whole turns are taken away there, and only the rest, at most half a turn, becomes an fp32
-// number (off by 2^-26 of a turn at most, 1e-7 of the result).
+// number; what that rounds off (up to 2^-26 of a turn, 1e-7 of the result) turns the sine and cosine to first order.
 //
 // 32768 tokens of 32 + 8 heads, d = 128: 671 MB in 134 us, 5.0 TB/s (a copy reaches 4.8); 3 x 5003 tokens of 12 + 4 heads 23 us for the kernel, 29 a
 // call.  64 single tokens: 6 us, the round trips of tail length, page and store.
@@ -146,7 +146,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotaryGeom g, int per) {
             const int pos = g.positions[(int64_t)axis * g.batch * g.n + token];
             const double w = (double)g.inv_freq[f], w1 = w * kTurn, w2 = fma(w, kTurn, -w1) + w * kTurnRest;
             const double turns = fma((double)pos, w2, fma((double)pos, w1, -rint((double)pos * w1)));
-            sincospif(2.f * (float)turns, &sn[i], &cs[i]);
+            const float part = (float)turns, rest = (float)((turns - (double)part) * 6.283185307179586477);
+            float s0, c0;
+            sincospif(2.f * part, &s0, &c0);
+            cs[i] = fmaf(-rest, s0, c0);
+            sn[i] = fmaf(rest, c0, s0);
             if (g.transpose) sn[i] = -sn[i];
         }
     }

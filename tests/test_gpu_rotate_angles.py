@@ -36,3 +36,14 @@ def test_far_positions_lose_nothing(start, freq):
     for g, v, slope in zip(got, want, reversed(want)):
         tol = 1.001 * 2 * np.pi * 2.0 ** -26 * (np.abs(slope) + 2.0 ** -24) + 4 * 2.0 ** -23 * np.abs(v)
         S.assert_within(torch.from_numpy(g), v, tol, "start %d, frequency %g" % (start, freq))
+
+
+@FAR
+@pytest.mark.parametrize("transpose", [0, 1])
+def test_the_angle_is_not_rounded_to_fp32(start, transpose):
+    """Sine and cosine are as near as fp32 holds them, those near 0 too: 4 units (2^-23) of the value, and what double
+    leaves open of the angle (2^-49 of a turn and less, 2^-40 allowed)."""
+    for freq in (1.0, 0.3):
+        got, want = sines_and_cosines(start, freq, transpose)
+        for g, v in zip(got, want):
+            S.assert_within(torch.from_numpy(g), v, 4 * 2.0 ** -23 * np.abs(v) + 2.0 ** -40, "start %d, frequency %g" % (start, freq))
