@@ -155,7 +155,8 @@ static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {
         pl.tail_parts = (int)parts;
         pl.tail_items = (units * parts + 7) / 8 * 8 * tiles;
     }
-    pl.c_out = std::max((float)(p->scale * 1.4426950408889634), 1e-37f);
+    // (never 0, with which a masked logit, -inf, would be no number: a scale of 0 becomes the smallest subnormal, no logit then counts)
+    pl.c_out = std::max((float)(p->scale * 1.4426950408889634), 0x1p-149f);
     const size_t rows = (size_t)all * p->n_kv_heads * (pl.prefix_parts + pl.tail_parts);
     pl.off_ms = align_up(sizeof(float) * rows * p->head_dim, 256);
     pl.bytes = align_up(pl.off_ms + 2 * sizeof(float) * rows, 256);
