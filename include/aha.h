@@ -497,7 +497,7 @@ typedef struct aha_shared {
     int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, prefixes, pools and out */
     int32_t n_prefixes;   /* 0..65535; 0: the prefix arguments are not looked at */
     int32_t prefix_cap;   /* <= 2^30 */
-    float scale;          /* >= 0, finite */
+    float scale;          /* 0 .. 2.3e38: finite, times log2(e) too */
     int32_t reserved;     /* must be 0 */
     int64_t q_stride[3];  /* elements: batch, head, token */
     int64_t out_stride[3];

@@ -8,6 +8,8 @@
 
 namespace aha {
 
+constexpr double kLog2e = 1.4426950408889634;
+
 // What the two kinds of geometry have in common.
 static int32_t check_heads(int batch, int rows, const char *rows_name, int q_heads, int kv_heads, int d, int dtype) {
     if (batch < 1 || rows < 1 || q_heads < 1 || kv_heads < 1)
@@ -113,7 +115,8 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
         return fail(AHA_ERR_INVALID_ARG, "n_prefixes must be >= 0, prefix_cap >= 1");
     if (p->n_prefixes > 65535 || (p->n_prefixes > 0 && p->prefix_cap > 1 << 30))
         return fail(AHA_ERR_UNSUPPORTED, "n_prefixes exceeds 65535 or prefix_cap 2^30");
-    if (!(p->scale >= 0.f) || isinf(p->scale)) return fail(AHA_ERR_INVALID_ARG, "scale must be finite and >= 0");
+    if (!(p->scale >= 0.f) || isinf((float)(p->scale * kLog2e)))
+        return fail(AHA_ERR_INVALID_ARG, "scale must be >= 0 and finite, times log2(e) too");
     if (p->reserved != 0) return fail(AHA_ERR_INVALID_ARG, "reserved must be 0");
     if (pg && (rc = check_pages(pg, p->n_kv_heads, p->dtype, p->head_dim, strides))) return rc;
     if (!strides) return AHA_OK;
@@ -156,7 +159,7 @@ static SharedPlan plan_shared(const aha_shared *p, const aha_pages *pages) {
         pl.tail_items = (units * parts + 7) / 8 * 8 * tiles;
     }
     // (never 0, with which a masked logit, -inf, would be no number: a scale of 0 becomes the smallest subnormal, no logit then counts)
-    pl.c_out = std::max((float)(p->scale * 1.4426950408889634), 0x1p-149f);
+    pl.c_out = std::max((float)(p->scale * kLog2e), 0x1p-149f);
     const size_t rows = (size_t)all * p->n_kv_heads * (pl.prefix_parts + pl.tail_parts);
     pl.off_ms = align_up(sizeof(float) * rows * p->head_dim, 256);
     pl.bytes = align_up(pl.off_ms + 2 * sizeof(float) * rows, 256);
