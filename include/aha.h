@@ -454,7 +454,8 @@ int32_t aha_rotate(const aha_rotary *p, const void *q, const void *k, const floa
  *            [0, tokens].  Rows from new_len[b] on are padding: nothing is read
  *            for them, their rows of q_out stay as they are.
  * A token before 0, behind the table's last page or in a hole is dropped.  No two
- * tokens of a call may have the same place; the place then holds one of the two.
+ * tokens of a call may have the same place: what both pools then hold there is
+ * unspecified (parts of one's rows and parts of the other's).
  */
 int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void *q,
                          const void *k, const void *v, const float *inv_freq,
