@@ -480,8 +480,8 @@ int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void
  *                before the first and behind the last entry have no prefix.
  *  k_prefix, v_prefix  [n_prefixes, n_kv_heads, prefix_cap, head_dim] by stride.
  *  pages, k_pages, v_pages, page_table, tail_len  the tails; all null: no tails.
- *  new_len       as for aha_append_paged; rows from new_len[b] on are neither read
- *                nor written in out and lse.
+ *  new_len       as for aha_append_paged; rows of q from new_len[b] on may hold anything
+ *                (their memory has to be there), those of out and lse stay as they are.
  *  lse           out, fp32 dense [batch, n_q_heads, q_len] or NULL: natural logarithm of
  *                sum_j exp(scale * q . K_j).
  * A row without a key gets zeros, and -inf in lse.  Keys and values that no row of the
