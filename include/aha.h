@@ -484,6 +484,8 @@ int32_t aha_append_paged(const aha_rotary *p, const aha_pages *pages, const void
  *                (their memory has to be there), those of out and lse stay as they are.
  *  lse           out, fp32 dense [batch, n_q_heads, q_len] or NULL: natural logarithm of
  *                sum_j exp(scale * q . K_j).
+ * The products' sums, the softmax and the joined outputs are fp32; with AHA_BF16 the weights are
+ * rounded to bf16 where they meet the values.
  * A row without a key gets zeros, and -inf in lse.  Keys and values that no row of the
  * sequence sees are not looked at: they may hold anything.  (Within a chunk, q_len > 1, the VALUES of
  * a sequence's new tokens have to be finite for its earlier ones.)
@@ -506,7 +508,11 @@ typedef struct aha_shared {
     int64_t v_stride[3];
 } aha_shared;
 
-/* `pages` may be null (no tails); of it only the sizes are looked at. */
+/*
+ * `pages` may be null (no tails); of it only the sizes are looked at.  The workspace holds head_dim + 2 floats
+ * per query row (batch * n_q_heads * q_len) and part of its keys: prefix and tail are one part each where the
+ * rows fill the chip (1.1 GB for 32768 rows of 32 heads, head_dim 128), up to 64 each where they do not.
+ */
 int32_t aha_shared_attention_workspace_bytes(const aha_shared *p, const aha_pages *pages,
                                              size_t *out_bytes);
 int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const void *q,

@@ -272,7 +272,6 @@ struct SharedGeom {
     PageGeom pages;
     int batch, n, Hq, Hkv, G, d, dtype;  // n: rows per sequence and head
     int n_prefixes, prefix_cap;
-    float scale;
 };
 // Work items: tiles of rows (prefixes: an upper bound, the sequences of each are known on the device) times KV heads (and sequences)
 // times parts of the keys; what lies where in the workspace.

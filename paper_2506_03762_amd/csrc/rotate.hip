@@ -182,7 +182,7 @@ static hipError_t launch_rotate_t(const RotaryGeom &g, hipStream_t st) {
     // 11.1, 11.2, 10.7, 13.1, 18.1).  Prompts of more than three tiles per CU whose heads' tokens lie together: nine heads or more
     // to a workgroup (bf16, d = 128; fp32 goes the same way: 20 heads with one, two, four workgroups to a tile 48.5, 50.2, 56.8 at 700 tiles, 58.0, 55.4, 62.3 at 780, 76.3,
     // 71.6, 80.2 at 1030; 40 heads 94.6, 96.0, 92.7; 113.5, 106.2, 102.6; 151.0, 143.3, 133.6; 8 heads 18.4, 23.8, 30.3 at 700, 29.2, 35.8, 42.2 at 1030; 72 heads
-    // with one, four, eight 270.2, 246.3, 232.9).  Where a token's heads lie together one workgroup is as good or better at all lengths (40 heads,
+    // with one, four, eight 270.2, 246.3, 232.9).  Where a token's heads lie together one workgroup is within 3 % of the best at such lengths (40 heads,
     // 1024 tiles, one, two, four 146.7, 149.6, 151.2).
     const bool head_major = g.Hq > 1 ? g.qs[1] > g.qs[2] : g.ks[1] > g.ks[2];
     const int64_t dealt = !APPEND && head_major && tiles > 3 * 256 ? heads / 9 : (384 + tiles - 1) / tiles;

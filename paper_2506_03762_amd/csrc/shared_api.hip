@@ -20,7 +20,7 @@ static int32_t check_heads(int batch, int rows, const char *rows_name, int q_hea
     return AHA_OK;
 }
 
-// A written tensor: rows that fall on each other are refused where that shows without their contents.
+// A written tensor: batches and heads a row or more apart (that the caller's axes do not overlap otherwise is up to them).
 static int32_t check_out_stride(const char *name, const int64_t s[3], int64_t n0, int64_t n1, int dtype, int d) {
     const int32_t rc = check_stride(name, s, dtype, d);
     if (rc) return rc;
@@ -130,7 +130,8 @@ static int32_t check_shared(const aha_shared *p, const aha_pages *pg, bool strid
 
 // Rows of a tile for about `rows` rows that see the same keys.  us of a call with tiles of 32 and of 128 rows: 64 rows of 8 heads, 16384 keys
 // 27.3, 36.2; 4 x 64 rows, 4096 keys, d = 64 34.8, 42.4; 128 rows of 8 heads 40.8, 44.1 for 16384 keys, 69.5, 58.1 for 32768; 128 rows of 32
-// heads 124.8, 89.4; with tiles of 32 and of 256: 192 rows of 8 heads 60.2, 50.2.
+// heads 124.8, 89.4; with tiles of 32 and of 256: 192 rows of 8 heads 60.2, 50.2.  Prefixes: the rows of an evenly filled one (which rows share
+// which prefix is known on the device alone), so that calls with room for many prefixes take small tiles, however few are in use.
 static int tile_rows(int dtype, int64_t rows) { return dtype != AHA_BF16 || rows <= 64 ? 32 : rows <= 128 ? 128 : 256; }
 // Parts of an item's keys: as many as fill the chip (two workgroups per CU, large tiles one) with `tiles` in each, large tiles of four steps at
 // least.
@@ -260,7 +261,7 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
     }
     g.pages = page_geom(pages, page_table, tail_len, new_len);
     g.batch = p->batch; g.n = p->q_len; g.Hq = p->n_q_heads; g.Hkv = p->n_kv_heads; g.G = g.Hq / g.Hkv;
-    g.d = p->head_dim; g.dtype = p->dtype; g.n_prefixes = p->n_prefixes; g.prefix_cap = p->prefix_cap; g.scale = p->scale;
+    g.d = p->head_dim; g.dtype = p->dtype; g.n_prefixes = p->n_prefixes; g.prefix_cap = p->prefix_cap;
     return hip_result(launch_shared_attention(g, pl, workspace, (hipStream_t)stream), "shared-prefix attention kernels");
 }
 

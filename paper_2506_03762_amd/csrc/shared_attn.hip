@@ -73,10 +73,13 @@ __device__ __forceinline__ void merge_waves(const SharedGeom &g, const SharedPla
 // ---- bf16, up to 32 rows ----
 // Four waves take blocks of 32 keys in turn, each with all rows: a stream of keys and values, bound by memory.  Per block and
 // wave: S^T = K Q^T and O^T += V^T P^T by v_mfma_f32_32x32x16_bf16, keys (channels) on M, rows on N, so that the accumulator elements of a
-// lane are the probabilities that it supplies to the second product.  Keys go to registers, values to LDS, both a block ahead: 128 KB
-// of requests per workgroup, two of them per CU.  64 sequences of four prefixes of 4096 tokens, tails of up to 1001: 203 MB from memory (each prefix once:
+// lane are the probabilities that it supplies to the second product.  Keys go to registers, values to LDS, both a block ahead: 64 KB
+// of requests per workgroup (d = 128), two of them per CU.  64 sequences of four prefixes of 4096 tokens, tails of up to 1001: 203 MB from memory (each prefix once:
 // the second tile of its 64 rows finds it in the L2) in 52 us, 3.9 TB/s; what is missing of 4.8 are the items' starts, 4 to 6 us each, and the last
 // tails.  8 sequences of one prefix of 2048: 9.4 us, a chain of five round trips.
+// The weights are rounded to bf16 for the second product, as the matrix core takes them beside bf16 values (their sum is of the unrounded ones, in fp32):
+// outputs are 0.0018 to 0.0023 from 64 bits, relative to their size, where a single rounding of the exact ones is 0.0017.  Weights in two
+// parts would double that product.
 template <int D>
 struct NarrowAttn {
     static constexpr int WAVES = 4, STEP = 32 * WAVES, CPR = D / 8, RPI = 64 / CPR, NI = 32 / RPI;
@@ -208,7 +211,9 @@ __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, Sha
 // ---- fp32 ----
 // The same on v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it): a lane's chunks of a key row and a query
 // row as in f32_tile.h; the second product takes the probabilities from the accumulators one element at a time, a
-// contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.
+// contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.  Beyond a few workgroups' latency
+// the loads bound it: a block's page, keys and values are requested one after the other, none ahead (2 x 64 rows x 4 heads, 4096 keys, d = 128: products
+// 7 of 49 us).
 // The dots of 32 keys and 32 rows in four chains of D / 4 products: eight, as in f32_tile.h, leave no room beside the outputs (d = 128, 8
 // sequences of one prefix of 2048 keys 26.3 us, so 21.6; 2 x 64 rows x 4 heads, 4096 keys 57.4, 49.5; d = 64 37.2, 29.0).
 template <int D>

@@ -9,7 +9,7 @@
 //   phase 1 of keys i:  S0(i+1) = K(i+1) Q0, O0 += V(i) P0(i)   beside   P1(i) = 2^(S1(i) - m1)
 //
 // so that one wave per SIMD keeps both busy; a second one would not fit its registers (two outputs of 64, queries 64, keys 32,
-// values 32, logits 32, probabilities 16).  A key or value fragment is read from LDS once for both row blocks, right behind its
+// values 32, logits 32, probabilities 16, rounded to bf16: shared_attn.hip).  A key or value fragment is read from LDS once for both row blocks, right behind its
 // last use, and waits in registers for 16 products: half of the reads of a wave with one row block, for which
 // LDS is as busy as the matrix core.
 //
@@ -307,6 +307,8 @@ __global__ __launch_bounds__(256, 1) void shared_wide_kernel(SharedGeom g, Share
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[0][ks], ks ? acc[0] : zero, 0, 0, 0);
         finish(0, 0);
+        // (one hole in an item sends all its blocks the long way: 4 x 256 rows of 32 heads, tails of 8192 alone 155 us without holes, 182
+        // with one in each tail)
         const int plain = holes ? 0 : (int)max((int64_t)0, min((int64_t)it.end, (int64_t)limit_min + 1) - it.begin) / A::KEYS;
         using P0 = std::integral_constant<int, 0>;
         using P1 = std::integral_constant<int, 1>;
