@@ -8,7 +8,7 @@
 // at 2^31), its whole turns are taken away there, and only the rest, at most half a turn, becomes an fp32
 // number; what that rounds off (up to 2^-26 of a turn, 1e-7 of the result) turns the sine and cosine to first order.
 //
-// 32768 tokens of 32 + 8 heads, d = 128: 671 MB in 134 us, 5.0 TB/s (a copy reaches 4.8); 3 x 5003 tokens of 12 + 4 heads 23 us for the kernel, 29 a
+// 32768 tokens of 32 + 8 heads, d = 128: 671 MB in 134 us, 5.0 TB/s (a copy reaches 4.8); 3 x 5003 tokens of 12 + 4 heads 26 us for the kernel, 29 a
 // call.  64 single tokens: 6 us, the round trips of tail length, page and store.
 #include <algorithm>
 
