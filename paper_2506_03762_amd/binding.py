@@ -451,6 +451,8 @@ class SharedAttention(_Described):
         heads then has to be given).  scale None: 1 / sqrt(d)."""
         if k_prefix is None and n_kv_heads is None:
             raise ValueError("neither prefixes nor n_kv_heads are given")
+        if (k_prefix is None) != (v_prefix is None):
+            raise ValueError("k_prefix and v_prefix must both be given or both be None")
         p = aha_shared(batch=q.size(0), q_len=q.size(2), n_q_heads=q.size(1), head_dim=q.size(3),
                        n_kv_heads=n_kv_heads if k_prefix is None else k_prefix.size(1),
                        dtype=_CODES.get(q.dtype, -1), scale=default_fixed_scale(q.size(3)) if scale is None else scale,
@@ -461,7 +463,7 @@ class SharedAttention(_Described):
             p.n_prefixes, p.prefix_cap = k_prefix.size(0), k_prefix.size(2)
             p.k_stride, p.v_stride = _view("k_prefix", k_prefix, q), _view("v_prefix", v_prefix, q)
         return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), q.dtype, ("q", q),
-                   ("k_prefix", k_prefix), ("v_prefix", None if k_prefix is None else v_prefix),
+                   ("k_prefix", k_prefix), ("v_prefix", v_prefix),
                    ("prefix_len", p.n_prefixes), ("prefix_first", p.n_prefixes + 1),
                    ("new_len", p.batch), ("out", out), ("lse", q.numel() // p.head_dim))
 

@@ -148,3 +148,10 @@ def test_workspace(calls):
         with pytest.raises(ValueError):
             attend(workspace)
     assert calls == ["aha_shared_attention"] * 2
+
+
+def test_one_half_of_a_prefix():
+    q, prefix = rows(2, 2, 3, 64), rows(1, 2, 50, 64)
+    for k, v in ((prefix, None), (None, prefix)):
+        with pytest.raises(ValueError):
+            B.SharedAttention.of(q, q, k, v, n_kv_heads=2)
