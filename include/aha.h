@@ -523,6 +523,134 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
                              const int32_t *new_len, void *out, float *lse, void *workspace,
                              size_t workspace_bytes, void *stream);
 
+/*
+ * ---- A batch of prompts and bounded caches in pages ---------------------------
+ *
+ * What carries a batch of prompts of different lengths into generation: the attention of
+ * whole prompts, the attention of single tokens over the paged cache, which keeps the
+ * running scores of the cached tokens, and the eviction from the paged cache by these scores.
+ * They keep the general rules above; lengths, tables and counts are read on the device, so that a
+ * captured call follows them.
+ */
+
+/*
+ * Causal attention of packed prompts.  The tokens first[s] .. first[s + 1] - 1 are prompt s:
+ *
+ *   out[t, h, :] = sum_j softmax_j(scale * q[t, h] . K_j) V_j,   j the tokens of t's prompt up to t.
+ *
+ *  q, out      [tokens, n_q_heads, head_dim] by stride; k, v [tokens, n_kv_heads, head_dim].
+ *  first       DEVICE int32 [sequences + 1], ascending, within [0, tokens]; equal ones: an empty
+ *              prompt.  Tokens before the first and behind the last entry belong to none: nothing of
+ *              theirs is looked at, their rows of out and lse stay as they are.
+ *  lse         out, fp32 dense [n_q_heads, tokens] or NULL: natural logarithm of
+ *              sum_j exp(scale * q . K_j).  The last `window` columns of a prompt are what
+ *              aha_prefill_scores_lse takes for it (scale_mode FIXED, the same scale).
+ * The products' sums and the softmax are fp32; with AHA_BF16 the weights are rounded to bf16 where they
+ * meet the values.  The VALUES of a prompt have to be finite (an infinite one reaches rows before it);
+ * keys may be anything, a row knows those that it sees.
+ */
+typedef struct aha_prompt {
+    int32_t tokens;       /* >= 1; tokens * n_q_heads <= 2^30 */
+    int32_t sequences;    /* 1..65535 */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads */
+    int32_t n_kv_heads;   /* <= 65535 */
+    int32_t head_dim;     /* 64 or 128 */
+    int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, k, v and out */
+    float scale;          /* 0 .. 2.3e38: finite, times log2(e) too */
+    int32_t reserved;     /* must be 0 */
+    int64_t q_stride[2];  /* elements: token, head */
+    int64_t k_stride[2];
+    int64_t v_stride[2];
+    int64_t out_stride[2];
+} aha_prompt;
+
+int32_t aha_prompt_attention_workspace_bytes(const aha_prompt *p, size_t *out_bytes);
+int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, const void *v,
+                             const int32_t *first, void *out, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
+ * Single tokens over paged caches with running scores, and eviction from them (the generation of
+ * Alg. 1 on a batch of caches of different lengths).
+ *
+ * Token j of sequence b has, for KV head h, its key and value in the pages, its running score in
+ * scores[b, h, j] and its position in pos[b, h, j].  A sequence has tail_len[b] tokens (as
+ * aha_append_paged counts them, the newest one last), clamped to what table and `slots` hold.  No page
+ * may be in the tables of two sequences whose tokens are evicted.
+ */
+typedef struct aha_paged {
+    int32_t batch;        /* batch * n_kv_heads <= 65535, batch * n_q_heads <= 2^22 */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads; not looked at by aha_paged_evict */
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* 64 or 128 */
+    int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, pools and out */
+    int32_t slots;        /* columns of scores and pos, <= 2^30; 0: aha_paged_attention without them */
+    int32_t budget;       /* B >= 1: k of the adaptive scale; tokens that a sequence keeps */
+    int32_t recent;       /* aha_paged_evict: 0 <= recent, sink and recent + sink <= budget */
+    int32_t sink;
+    int32_t scale_mode;   /* AHA_SCALE_FIXED | AHA_SCALE_ADAPTIVE: scale of the accumulated weights */
+    float scale;          /* of the output's weights: 0 .. 2.3e38, finite, times log2(e) too */
+    float fixed_scale;    /* likewise, of the accumulated ones */
+    float lambda_floor;   /* as in aha_params; < 0: 1 / sqrt(head_dim) */
+    int32_t reserved;     /* must be 0 */
+    int64_t q_stride[2];  /* elements: batch, head (aha_paged_attention) */
+    int64_t out_stride[2];
+    int64_t scores_stride[2];
+    int64_t pos_stride[2];
+    int64_t scores_out_stride[2]; /* aha_paged_evict */
+    int64_t pos_out_stride[2];
+} aha_paged;
+
+/*
+ * One generation step's attention:
+ *
+ *   out[b, h, :] = sum_j softmax_j(scale * q[b, h] . K_j) V_j,   j < tail_len[b] and in a page,
+ *   scores[b, kv, j] += sum_{h in group(kv)} softmax_j(lambda_b * q[b, h] . K_j).
+ *
+ * lambda_b is what scale_mode gives a row that has seen seen[b] tokens (Sec. 4.2), k the budget.  The
+ * newest token's score starts from 0, whatever scores holds there, and its position becomes
+ * seen[b] - 1.  Scores of tokens in holes stay as they are, the newest's is 0 then.
+ *
+ *  q, out      [batch, n_q_heads, head_dim] by stride.
+ *  seen        DEVICE int32 [batch] or NULL (tail_len): tokens that a sequence has seen, the evicted ones
+ *              and the newest counted.
+ *  scores, pos in place, [batch, n_kv_heads, slots] by stride; pos may be null; both null: slots 0.
+ *  lse         out, fp32 dense [batch, n_q_heads] or NULL: natural logarithm of sum_j exp(scale * q . K_j).
+ * A row without a key gets zeros, and -inf in lse.
+ * The workspace holds head_dim + 4 floats per row and part of its keys (up to 64), and with scores
+ * 4 bytes per row and column of scores.
+ */
+int32_t aha_paged_attention_workspace_bytes(const aha_paged *p, const aha_pages *pages,
+                                            size_t *out_bytes);
+int32_t aha_paged_attention(const aha_paged *p, const aha_pages *pages, const void *q,
+                            const void *k_pages, const void *v_pages, const int32_t *page_table,
+                            const int32_t *tail_len, const int32_t *seen, float *scores,
+                            int32_t *pos, void *out, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/*
+ * Brings every sequence back to its budget: len_out[b] = min(tail_len[b], budget) tokens stay.  For each KV head
+ * those of the smallest scores go (ties: the highest position first, of equal positions the last place; a NaN
+ * counts as smallest).  Positions >= seen[b] - recent and < sink go last (which, with different positions, is
+ * never).  The tokens that stay and lie at or behind len_out[b] move, in order, into the places below it that
+ * became free, in order; all others stay where they are.
+ *
+ *  scores, pos   [batch, n_kv_heads, slots] by stride; pos null: token j has position j (a prompt's scores
+ *                as aha_prefill_scores leaves them).
+ *  seen          DEVICE int32 [batch] or NULL (tail_len).
+ *  k_pages, v_pages  in place.
+ *  scores_out, pos_out  out: what belongs to the tokens now in places below len_out[b]; places behind stay as
+ *                they are.  Either may be its input (same pointer and strides); otherwise they must not overlap.
+ *  len_out       out, DEVICE int32 [batch]; not tail_len.
+ * A sequence with a hole among its pages keeps all its tokens.
+ */
+int32_t aha_paged_evict_workspace_bytes(const aha_paged *p, const aha_pages *pages, size_t *out_bytes);
+int32_t aha_paged_evict(const aha_paged *p, const aha_pages *pages, const float *scores,
+                        const int32_t *pos, void *k_pages, void *v_pages, const int32_t *page_table,
+                        const int32_t *tail_len, const int32_t *seen, float *scores_out,
+                        int32_t *pos_out, int32_t *len_out, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
 /* Thread-local description of the last error returned on this thread. */
 const char *aha_last_error(void);
 

@@ -35,7 +35,10 @@ EXPORTS = ("aha_workspace_bytes", "aha_prefill_scores", "aha_prefill_scores_lse"
            "aha_prefill_window_attention", "aha_select_topk",
            "aha_compact_kv", "aha_decode_step", "aha_decode_step_static", "aha_profile_events",
            "aha_exchange_looks", "aha_rotate", "aha_append_paged",
-           "aha_shared_attention_workspace_bytes", "aha_shared_attention", "aha_last_error",
+           "aha_shared_attention_workspace_bytes", "aha_shared_attention",
+           "aha_prompt_attention_workspace_bytes", "aha_prompt_attention",
+           "aha_paged_attention_workspace_bytes", "aha_paged_attention",
+           "aha_paged_evict_workspace_bytes", "aha_paged_evict", "aha_last_error",
            "aha_version")
 
 
@@ -79,6 +82,20 @@ class aha_shared(ctypes.Structure):
             "q_stride", "out_stride", "k_stride", "v_stride")]
 
 
+class aha_prompt(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "sequences", "n_q_heads", "n_kv_heads", "head_dim", "dtype")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64 * 2) for n in (
+            "q_stride", "k_stride", "v_stride", "out_stride")]
+
+
+class aha_paged(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "slots", "budget", "recent", "sink", "scale_mode")] + [
+        (n, ctypes.c_float) for n in ("scale", "fixed_scale", "lambda_floor")] + [("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_int64 * 2) for n in ("q_stride", "out_stride", "scores_stride", "pos_stride", "scores_out_stride",
+                                          "pos_out_stride")]
+
+
 _lib = None
 
 
@@ -112,6 +129,13 @@ def load() -> ctypes.CDLL:
     lib.aha_append_paged.argtypes = [rp, gp] + [vp] * 13
     lib.aha_shared_attention_workspace_bytes.argtypes = [sp, gp, ctypes.POINTER(sz)]
     lib.aha_shared_attention.argtypes = [sp, gp] + [vp] * 13 + [sz, vp]
+    mp, cp = ctypes.POINTER(aha_prompt), ctypes.POINTER(aha_paged)
+    lib.aha_prompt_attention_workspace_bytes.argtypes = [mp, ctypes.POINTER(sz)]
+    lib.aha_prompt_attention.argtypes = [mp] + [vp] * 7 + [sz, vp]
+    lib.aha_paged_attention_workspace_bytes.argtypes = [cp, gp, ctypes.POINTER(sz)]
+    lib.aha_paged_attention.argtypes = [cp, gp] + [vp] * 11 + [sz, vp]
+    lib.aha_paged_evict_workspace_bytes.argtypes = [cp, gp, ctypes.POINTER(sz)]
+    lib.aha_paged_evict.argtypes = [cp, gp] + [vp] * 11 + [sz, vp]
     for name in EXPORTS[:-2]:
         getattr(lib, name).restype = i32
     lib.aha_last_error.restype = ctypes.c_char_p
@@ -344,7 +368,8 @@ def default_fixed_scale(head_dim: int) -> float:
 
 _CODES = {torch.float32: AHA_F32, torch.bfloat16: AHA_BF16}
 # what has no strides of its own: element types
-_DENSE = dict.fromkeys(("pair_axis", "positions", "page_table", "tail_len", "new_len", "prefix_len", "prefix_first"), torch.int32)
+_DENSE = dict.fromkeys(("pair_axis", "positions", "page_table", "tail_len", "new_len", "prefix_len", "prefix_first", "first", "seen",
+                        "len_out"), torch.int32)
 _DENSE.update(inv_freq=torch.float32, lse=torch.float32)
 
 
@@ -362,13 +387,14 @@ class _Described:
     in which a call takes them: names, element types, numbers of elements (dense ones) or shapes and strides."""
 
     def __init__(self, struct, rows, dtype, *tensors):
-        """tensors: name and number of elements, or name and the tensor that is described (None: not given)."""
+        """tensors: name and number of elements, or name, the tensor that is described (None: not given) and, where it is not
+        `dtype`, its element type."""
         self._as_parameter_ = ctypes.byref(struct)
         self.struct, self.rows = struct, rows
         self.tensors = tuple(
             (name, _DENSE[name], t, None, None) if name in _DENSE else
-            (name, dtype, None, (), ()) if t is None else (name, dtype, None, t.shape, t.stride())
-            for name, t in tensors)
+            (name, *(own or (dtype,)), None, *(((), ()) if t is None else (t.shape, t.stride())))
+            for name, t, *own in tensors)
 
 
 def _same_places(t, shape, stride):
@@ -525,3 +551,147 @@ def aha_shared_attention(p: SharedAttention, cache: Optional[Pages], q, k_prefix
         raise ValueError("workspace: not a contiguous tensor on the current device")
     tails = at[8:] if cache is not None else [_ptr(t) for t in (k_pages, v_pages, page_table, tail_len)]
     _check((_lib or load()).aha_shared_attention(p, cache, *at[:5], *tails, *at[5:8], *_ws(workspace), _stream()))
+
+
+# ---- a batch of prompts and bounded caches in pages ----
+
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """Strides (first two axes) of a [., heads, d] view whose channels are contiguous."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.size(2) > 1) or t.dtype not in _CODES:
+        raise ValueError("%s must be a 3-dimensional fp32 or bf16 view with contiguous channels" % name)
+    if like is not None and (t.dtype != like.dtype or t.size(2) != like.size(2)):
+        raise ValueError("%s has another dtype or head size" % name)
+    return (ctypes.c_int64 * 2)(*t.stride()[:2])
+
+
+def _slots(name: str, t: torch.Tensor, dtype, shape=None):
+    """Strides (first two axes) of a [b, Hkv, slots] view whose last axis is contiguous."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.size(2) > 1) or t.dtype is not dtype:
+        raise ValueError("%s must be a 3-dimensional view of %s with contiguous slots" % (name, dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s has another shape than %s" % (name, tuple(shape)))
+    return (ctypes.c_int64 * 2)(*t.stride()[:2])
+
+
+class PromptAttention(_Described):
+    """Description of an attention of packed prompts (aha_prompt)."""
+
+    @classmethod
+    def of(cls, q, k, v, out, first, scale: Optional[float] = None) -> "PromptAttention":
+        """For q and out [tokens, Hq, d], k and v [tokens, Hkv, d] (views by stride) and first [prompts + 1].  scale None:
+        1 / sqrt(d)."""
+        p = aha_prompt(tokens=q.size(0), sequences=first.numel() - 1, n_q_heads=q.size(1), n_kv_heads=k.size(1),
+                       head_dim=q.size(2), dtype=_CODES.get(q.dtype, -1),
+                       scale=default_fixed_scale(q.size(2)) if scale is None else scale, q_stride=_rows("q", q),
+                       k_stride=_rows("k", k, q), v_stride=_rows("v", v, q), out_stride=_rows("out", out, q))
+        if q.shape != out.shape or k.shape != v.shape or q.size(0) != k.size(0):
+            raise ValueError("q and out, or k and v, have different shapes, or q and k other tokens")
+        return cls(p, None, q.dtype, ("q", q), ("k", k), ("v", v), ("first", first.numel()), ("out", out),
+                   ("lse", q.size(0) * q.size(1)))
+
+
+def prompt_attention_workspace_bytes(p: PromptAttention) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().aha_prompt_attention_workspace_bytes(p, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_prompt_workspace(p: PromptAttention, device="cuda") -> torch.Tensor:
+    return torch.empty(max(prompt_attention_workspace_bytes(p), 256), dtype=torch.uint8, device=device)
+
+
+def aha_prompt_attention(p: PromptAttention, q, k, v, first, out, lse, workspace):
+    """out [tokens, Hq, d], lse [Hq, tokens] (fp32 or None) <- causal attention of the packed prompts first[s] .. first[s + 1] - 1."""
+    at = _pointers(p.tensors, (q, k, v, first, out, lse))
+    _check((_lib or load()).aha_prompt_attention(p, *at, *_own_ws(workspace), _stream()))
+
+
+def _own_ws(workspace):
+    """Pointer and size of a workspace, once it is a contiguous tensor on the current device."""
+    if workspace is not None and (workspace.get_device() != torch._C._cuda_getDevice() or not workspace.is_contiguous()):
+        raise ValueError("workspace: not a contiguous tensor on the current device")
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+class PagedAttention(_Described):
+    """Description of a generation step's attention over paged caches (aha_paged)."""
+
+    @classmethod
+    def of(cls, q, out, scores=None, pos=None, *, n_kv_heads: Optional[int] = None, scale: Optional[float] = None, budget: int = 1,
+           scale_mode: int = AHA_SCALE_ADAPTIVE, fixed_scale: float = 0.0, lambda_floor: float = -1.0) -> "PagedAttention":
+        """For q and out [b, Hq, d] views, running scores and positions [b, Hkv, slots] (pos or both may be None; without scores the number
+        of KV heads has to be given).  scale None: 1 / sqrt(d)."""
+        if scores is None and (n_kv_heads is None or pos is not None):
+            raise ValueError("without scores n_kv_heads has to be given, and no pos")
+        p = aha_paged(batch=q.size(0), n_q_heads=q.size(1), n_kv_heads=n_kv_heads if scores is None else scores.size(1),
+                      head_dim=q.size(2), dtype=_CODES.get(q.dtype, -1), slots=0 if scores is None else scores.size(2),
+                      budget=budget, scale_mode=scale_mode, fixed_scale=fixed_scale, lambda_floor=lambda_floor,
+                      scale=default_fixed_scale(q.size(2)) if scale is None else scale,
+                      q_stride=_rows("q", q), out_stride=_rows("out", out, q))
+        if q.shape != out.shape or (scores is not None and scores.size(0) != q.size(0)):
+            raise ValueError("q and out have different shapes, or scores another batch")
+        if scores is not None:
+            p.scores_stride = _slots("scores", scores, torch.float32)
+        if pos is not None:
+            p.pos_stride = _slots("pos", pos, torch.int32, scores.shape)
+        return cls(p, (p.batch, p.n_kv_heads, p.head_dim, q.dtype), q.dtype, ("q", q), ("seen", p.batch),
+                   ("scores", scores, torch.float32), ("pos", pos, torch.int32), ("out", out), ("lse", p.batch * p.n_q_heads))
+
+
+def paged_attention_workspace_bytes(p: PagedAttention, cache: Pages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().aha_paged_attention_workspace_bytes(p, cache, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_paged_workspace(p: PagedAttention, cache: Pages, device="cuda") -> torch.Tensor:
+    return torch.empty(max(paged_attention_workspace_bytes(p, cache), 256), dtype=torch.uint8, device=device)
+
+
+def aha_paged_attention(p: PagedAttention, cache: Pages, q, k_pages, v_pages, page_table, tail_len, seen, scores, pos, out, lse,
+                        workspace):
+    """out [b, Hq, d], lse [b, Hq] (fp32 or None) <- attention of one new token of every sequence over its pages; scores [b, Hkv, slots] +=
+    the weights that the cached tokens get, the newest one's score and position are set."""
+    _check_same(p, cache)
+    at = _pointers(p.tensors + cache.tensors[:4], (q, seen, scores, pos, out, lse, k_pages, v_pages, page_table, tail_len))
+    _check((_lib or load()).aha_paged_attention(p, cache, at[0], *at[6:], *at[1:6], *_own_ws(workspace), _stream()))
+
+
+class PagedEviction(_Described):
+    """Description of an eviction from paged caches (aha_paged)."""
+
+    @classmethod
+    def of(cls, scores, pos, scores_out, pos_out, cache: Pages, *, budget: int, recent: int = 0, sink: int = 0) -> "PagedEviction":
+        """For running scores and positions [b, Hkv, slots] (pos None: token j has position j) and what they become; an output may be
+        its input."""
+        batch, heads, d, dtype = cache.rows
+        if scores.shape[:2] != (batch, heads):
+            raise ValueError("scores are not of the cache's sequences and KV heads")
+        p = aha_paged(batch=batch, n_q_heads=heads, n_kv_heads=heads, head_dim=d, dtype=_CODES[dtype], slots=scores.size(2), budget=budget,
+                      recent=recent, sink=sink, scores_stride=_slots("scores", scores, torch.float32),
+                      scores_out_stride=_slots("scores_out", scores_out, torch.float32, scores.shape),
+                      pos_out_stride=_slots("pos_out", pos_out, torch.int32, scores.shape))
+        if pos is not None:
+            p.pos_stride = _slots("pos", pos, torch.int32, scores.shape)
+        return cls(p, cache.rows, dtype, ("scores", scores, torch.float32), ("pos", pos, torch.int32), ("seen", batch),
+                   ("scores_out", scores_out, torch.float32), ("pos_out", pos_out, torch.int32), ("len_out", batch))
+
+
+def paged_evict_workspace_bytes(p: PagedEviction, cache: Pages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().aha_paged_evict_workspace_bytes(p, cache, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_evict_workspace(p: PagedEviction, cache: Pages, device="cuda") -> torch.Tensor:
+    return torch.empty(max(paged_evict_workspace_bytes(p, cache), 256), dtype=torch.uint8, device=device)
+
+
+def aha_paged_evict(p: PagedEviction, cache: Pages, scores, pos, k_pages, v_pages, page_table, tail_len, seen, scores_out, pos_out,
+                    len_out, workspace):
+    """The sequences brought back to their budget: len_out [b] tokens stay, whose scores and positions go to scores_out and pos_out, whose
+    keys and values to the places below len_out."""
+    _check_same(p, cache)
+    at = _pointers(p.tensors + cache.tensors[:4], (scores, pos, seen, scores_out, pos_out, len_out, k_pages, v_pages, page_table,
+                                                   tail_len))
+    _check((_lib or load()).aha_paged_evict(p, cache, *at[:2], *at[6:], *at[2:6], *_own_ws(workspace), _stream()))

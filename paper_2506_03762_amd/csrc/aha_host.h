@@ -288,4 +288,59 @@ hipError_t launch_shared_attention(const SharedGeom &g, const SharedPlan &pl, vo
 // The items of `pl` in tiles of 128 or 256 rows (bf16).
 hipError_t launch_shared_wide(const SharedGeom &g, const SharedPlan &pl, int rows, float *part_o, float2 *part_ms, hipStream_t st);
 
+// prompt_attn.hip
+// Causal attention of packed prompts: work items are tiles of a prompt's consecutive rows of one query head.
+struct PromptGeom {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    const int32_t *first;
+    int64_t qs[2], ks[2], vs[2], os[2];  // element strides: token, head
+    int tokens, sequences, Hq, Hkv, G, d, dtype;
+    float c_out;  // scale times log2(e), above 0
+};
+struct PromptPlan {
+    int rows;       // of a tile
+    int64_t tiles;  // at most (the prompts' lengths are known on the device)
+    int64_t items;  // workgroups
+};
+hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
+
+// paged_attn.hip
+// One new token of every sequence over its pages, and the running scores.
+struct PagedGeom {
+    const void *q, *kt, *vt;
+    void *out;
+    float *lse, *scores;
+    int32_t *pos;
+    const int32_t *seen;
+    int64_t qs[2], os[2], ss[2], ps[2];  // element strides: batch, head
+    PageGeom pages;
+    int batch, Hq, Hkv, G, d, dtype, slots, budget, scale_mode;
+    float c_out, fixed_scale, lambda_floor;  // c_out: scale times log2(e), above 0
+};
+struct PagedPlan {
+    int tiles, parts;   // of 32 rows of a (sequence, KV head), of its keys
+    int64_t items, ld;  // workgroups; floats of a row of dots
+    size_t off_ms, off_ms2, off_dots, bytes;  // behind the partial outputs: references and sums, of the output's weights and of the scores'
+};
+hipError_t launch_paged_attention(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st);
+
+// paged_evict.hip
+struct EvictGeom {
+    const float *scores;
+    const int32_t *pos, *seen;
+    void *kt, *vt;
+    float *scores_out;
+    int32_t *pos_out, *len_out;
+    int64_t ss[2], ps[2], so[2], po[2];  // element strides: batch, head
+    PageGeom pages;
+    int batch, Hkv, d, dtype, slots, budget, recent, sink;
+};
+struct EvictPlan {
+    int moves;          // of a (sequence, KV head), at most
+    size_t off_moves, bytes;  // behind the counts: (to, from) of every move
+};
+hipError_t launch_paged_evict(const EvictGeom &g, const EvictPlan &pl, void *ws, hipStream_t st);
+
 }  // namespace aha

@@ -1,0 +1,219 @@
+// Attention of one new token of every sequence over its paged cache, and the running scores of the cached tokens:
+//
+//   out = sum_j softmax_j(scale q . K_j) V_j        F_j += sum_g softmax_j(lambda q_g . K_j)
+//
+// in two launches.  The first takes the keys of a (sequence, KV head) in parts: the rows of its query heads, padded to a tile of 32, in one pass
+// over the part's keys and values (narrow_tile.h), which leaves the products, a partial output and the sums of both softmaxes, relative
+// to references of their own, in the workspace.  The second joins the parts: outputs by row, scores by range of keys.
+#include <limits.h>
+
+#include "narrow_tile.h"
+
+namespace aha {
+
+// The tokens of sequence b.
+__device__ __forceinline__ int tokens_of(const PagedGeom &g, int b) {
+    const int64_t room = (int64_t)g.pages.table_width << g.pages.page_shift;
+    return max(0, (int)min((int64_t)g.pages.tail_len[b], g.slots > 0 ? min(room, (int64_t)g.slots) : room));
+}
+// Scale of the accumulated weights, times log2(e); above 0, with which a masked product, -inf, is no number otherwise.
+__device__ __forceinline__ float score_scale(const PagedGeom &g, int b) {
+    const int c = max(1, (g.seen ? g.seen : g.pages.tail_len)[b]);
+    return fmaxf(row_scale_log2(g.scale_mode, g.fixed_scale, g.lambda_floor, c, g.budget, g.d), 0x1p-149f);
+}
+// Number of the partial result of row gi of (sequence, KV head) z.
+__device__ __forceinline__ int64_t paged_partial(const PagedGeom &g, const PagedPlan &pl, int z, int part, int gi) {
+    return ((int64_t)z * pl.parts + part) * g.G + gi;
+}
+
+template <class T, int D>
+struct PagedLds;
+template <int D>
+struct PagedLds<__bf16, D> {
+    static constexpr size_t bytes = NarrowRows<D>::stage_bytes > WaveMerge<D>::bytes ? NarrowRows<D>::stage_bytes : WaveMerge<D>::bytes;
+};
+template <int D>
+struct PagedLds<float, D> {
+    static constexpr size_t q_bytes = (size_t)32 * f32_ld(D) * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
+};
+
+template <class T, int D>
+__global__ __launch_bounds__(256, 2) void paged_part_kernel(PagedGeom g, PagedPlan pl, float *part_o, float2 *part_ms, float2 *part_ms2, float *dots) {
+    constexpr int STEP = NarrowRows<D>::STEP;
+    __shared__ __attribute__((aligned(1024))) char smem[PagedLds<T, D>::bytes];
+    __shared__ float2 s_ms2[4][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    // (sequence, KV head) by part by tile
+    const int id = blockIdx.x, tile = id % pl.tiles, part = id / pl.tiles % pl.parts, z = id / pl.tiles / pl.parts;
+    const int b = z / g.Hkv, h = z % g.Hkv, row0 = tile * 32, rows = min(32, g.G - row0);
+    const int len = uniform(tokens_of(g, b)), steps = (len + STEP - 1) / STEP;
+    const bool live = col < rows;
+    const int gi = row0 + min(col, rows - 1), hq = h * g.G + gi;
+    KeyPlaces<T> keys;
+    keys.in_pages(g.pages, g.kt, g.vt, b, h);
+    keys.begin = (int)((int64_t)part * steps / pl.parts) * STEP;
+    keys.end = min(len, (int)((int64_t)(part + 1) * steps / pl.parts) * STEP);
+    if (keys.begin >= keys.end) {
+        if (tid < rows) {
+            part_ms[paged_partial(g, pl, z, part, row0 + tid)] = make_float2(-INFINITY, 0.f);
+            if (dots) part_ms2[paged_partial(g, pl, z, part, row0 + tid)] = make_float2(-INFINITY, 0.f);
+        }
+        return;
+    }
+    const T *q = (const T *)g.q + b * g.qs[0] + hq * g.qs[1];
+    float *to = dots + ((int64_t)b * g.Hq + hq) * pl.ld + 4 * hf;
+    const float lam = dots ? score_scale(g, b) : 0.f;
+    float m2 = -INFINITY, s2 = 0.f;
+    auto block = [&](int kb, const f32x16 &acc) {
+        if (!dots) return;
+        if (live) {
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) *(f32x4 *)(to + kb + 2 * v) = f32x4{acc[v], acc[v + 1], acc[v + 2], acc[v + 3]};
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[v]);
+        const float mn = fmaxf(m2, top * lam), ref = mn == -INFINITY ? 0.f : mn;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sum[v & 3] += fast_exp2(fmaf(acc[v], lam, -ref));
+        s2 = s2 * fast_exp2(m2 - ref) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        m2 = mn;
+    };
+    f32x16 O[D / 32];
+    float m, s;
+    no_rows_yet(O, m, s);
+    if constexpr (sizeof(T) == 2) {
+        bf16x8 qf[D / 16];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            qf[ks] = *(const bf16x8 *)(q + hf * 8 + ks * 16);
+            if (!live) qf[ks] = bf16x8{};
+        }
+        narrow_sweep<D>(keys, qf, INT_MAX, g.c_out, smem, lane, wave, O, m, s, block);
+    } else {
+        float *sQ = (float *)smem;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
+            const int c = wave * (D / 4) + i * 8 + hf * 4;
+            f32x4 x = *(const f32x4 *)(q + c);
+            if (!live) x = f32x4{};
+            *(f32x4 *)(sQ + col * f32_ld(D) + c) = x;
+        }
+        __syncthreads();
+        f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, INT_MAX, g.c_out, lane, wave, O, m, s, block);
+    }
+    if (dots) {  // the sums of the half-waves, later those of the waves
+        const float M = combine_lane_xor<32>(m2, OpMax{}), ref = M == -INFINITY ? 0.f : M;
+        const float all = combine_lane_xor<32>(s2 * fast_exp2(m2 - ref), OpSum{});
+        if (lane < 32) s_ms2[wave][lane] = make_float2(M, all);
+    }
+    meet_waves<D>(
+        rows, live, O, m, s, smem, lane, wave,
+        [&](float M, float all) {
+            const int64_t p = paged_partial(g, pl, z, part, gi);
+            part_ms[p] = make_float2(M, all);
+            if (!dots) return;
+            float M2 = -INFINITY, all2 = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) M2 = fmaxf(M2, s_ms2[w][col].x);
+            const float ref = M2 == -INFINITY ? 0.f : M2;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) all2 = fmaf(fast_exp2(s_ms2[w][col].x - ref), s_ms2[w][col].y, all2);
+            part_ms2[p] = make_float2(M2, all2);
+        },
+        [&](int r, int ch, const f32x4 &o) { *(f32x4 *)(part_o + paged_partial(g, pl, z, part, row0 + r) * D + ch) = o; });
+}
+
+// ---- joining ----
+// Workgroups of a (sequence, KV head): the first `g.G` / rows ones join output rows, the others take kJoinKeys keys of the scores each.
+constexpr int kJoinKeys = 1024, kMaxGroup = 1024;
+template <class T, int D, int SP>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedGeom g, PagedPlan pl, const float *part_o, const float2 *part_ms,
+                                                         const float2 *part_ms2, const float *dots) {
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * SP), U = 4;
+    const int z = blockIdx.y, b = z / g.Hkv, h = z % g.Hkv, tid = threadIdx.x, out_wgs = (g.G + ROWS - 1) / ROWS;
+    if ((int)blockIdx.x < out_wgs) {
+        const int ch = tid % TPR * 4, sp = tid / TPR % SP, gi = blockIdx.x * ROWS + tid / (TPR * SP);
+        JoinState x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+        if (gi < g.G) {
+            for (int p = sp; p < pl.parts; p += U * SP) {
+                float2 ms[U];
+                f32x4 o[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {  // (past the last part: the first of these again)
+                    const int64_t i = paged_partial(g, pl, z, p + u * SP < pl.parts ? p + u * SP : p, gi);
+                    ms[u] = part_ms[i];
+                    o[u] = *(const f32x4 *)(part_o + i * D + ch);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (p + u * SP < pl.parts) x.add(ms[u].x, ms[u].y, o[u]);
+            }
+        }
+        if constexpr (SP > 1) {
+            __shared__ f32x4 s_o[256];
+            __shared__ float2 s_ms[256];
+            s_o[tid] = x.o;
+            s_ms[tid] = make_float2(x.m, x.s);
+            __syncthreads();
+            if (sp) return;
+#pragma unroll
+            for (int u = 1; u < SP; ++u) x.add(s_ms[tid + u * TPR].x, s_ms[tid + u * TPR].y, s_o[tid + u * TPR]);
+        }
+        if (gi >= g.G) return;
+        const int hq = h * g.G + gi;
+        store_output((T *)g.out + b * g.os[0] + hq * g.os[1] + ch, x.o, x.s == 0.f ? 0.f : 1.f / x.s);
+        if (g.lse && ch == 0) g.lse[(int64_t)b * g.Hq + hq] = x.s == 0.f ? -INFINITY : (x.m + log2f(x.s)) * kLn2;
+        return;
+    }
+    // ---- scores ----
+    const int len = tokens_of(g, b), k0 = (blockIdx.x - out_wgs) * kJoinKeys;
+    if (k0 >= len) return;
+    __shared__ float2 norm[kMaxGroup];  // of every row: reference, 1 / sum
+    const int lane = tid & 63;
+    for (int gi = tid >> 6; gi < g.G; gi += 4) {  // (up to 64 parts, one per lane)
+        const float2 ms = lane < pl.parts ? part_ms2[paged_partial(g, pl, z, lane, gi)] : make_float2(-INFINITY, 0.f);
+        const float M = wave_max(ms.x), ref = M == -INFINITY ? 0.f : M, all = wave_sum(fast_exp2(ms.x - ref) * ms.y);
+        if (lane == 0) norm[gi] = make_float2(ref, all > 0.f ? 1.f / all : all == 0.f ? 0.f : all);  // (NaN stays)
+    }
+    __syncthreads();
+    const float lam = score_scale(g, b);
+    const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld;
+    float *F = g.scores + b * g.ss[0] + h * g.ss[1];
+    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
+    for (int j = k0 + tid; j < min(len, k0 + kJoinKeys); j += 256) {
+        float w = 0.f;
+        for (int gi = 0; gi < g.G; ++gi) w += fast_exp2(fmaf(x[gi * pl.ld + j], lam, -norm[gi].x)) * norm[gi].y;
+        const int page = table[j >> g.pages.page_shift];
+        const bool there = page >= 0 && page < g.pages.n_pages;
+        if (j == len - 1) F[j] = there ? w : 0.f;
+        else if (there) F[j] += w;
+        if (j == len - 1 && g.pos) g.pos[b * g.ps[0] + h * g.ps[1] + j] = (g.seen ? g.seen : g.pages.tail_len)[b] - 1;
+    }
+}
+
+template <class T, int D>
+static hipError_t launch_paged_t(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st) {
+    float *part_o = (float *)ws, *dots = g.slots > 0 ? (float *)((char *)ws + pl.off_dots) : nullptr;
+    float2 *part_ms = (float2 *)((char *)ws + pl.off_ms), *part_ms2 = (float2 *)((char *)ws + pl.off_ms2);
+    hipLaunchKernelGGL((paged_part_kernel<T, D>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int score_wgs = g.slots > 0 ? (int)((pl.ld + kJoinKeys - 1) / kJoinKeys) : 0;
+    auto join = [&](auto kernel, int rows) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((g.G + rows - 1) / rows + score_wgs), g.batch * g.Hkv), dim3(256), 0, st, g, pl, part_o, part_ms,
+                           part_ms2, dots);
+    };
+    // (up to four parts are in flight at once anyway)
+    if (pl.parts <= 4) join(paged_join_kernel<T, D, 1>, 256 / (D / 4));
+    else join(paged_join_kernel<T, D, 8>, 256 / (D / 4 * 8));
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_attention(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st) {
+    if (g.dtype == AHA_BF16) return g.d == 64 ? launch_paged_t<__bf16, 64>(g, pl, ws, st) : launch_paged_t<__bf16, 128>(g, pl, ws, st);
+    return g.d == 64 ? launch_paged_t<float, 64>(g, pl, ws, st) : launch_paged_t<float, 128>(g, pl, ws, st);
+}
+
+}  // namespace aha

@@ -1,0 +1,79 @@
+// Causal attention of packed prompts:
+//
+//   out_t = sum_{j <= t} softmax_j(scale q_t . K_j) V_j,   j in t's prompt
+//
+// in one pass over a row's keys with a running reference m (narrow_tile.h).  A workgroup takes a tile of consecutive rows of one query head and
+// all keys up to its last row.
+#include <limits.h>
+
+#include "narrow_tile.h"
+#include "prompt_tiles.h"
+
+namespace aha {
+
+template <class T, int D>
+struct PromptLds;
+template <int D>
+struct PromptLds<__bf16, D> {
+    static constexpr size_t bytes = NarrowRows<D>::stage_bytes > WaveMerge<D>::bytes ? NarrowRows<D>::stage_bytes : WaveMerge<D>::bytes;
+};
+template <int D>
+struct PromptLds<float, D> {
+    static constexpr size_t q_bytes = (size_t)32 * f32_ld(D) * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
+};
+
+// ---- tiles of 32 rows ----
+template <class T, int D>
+__global__ __launch_bounds__(256, 2) void prompt_narrow_kernel(PromptGeom g) {
+    __shared__ __attribute__((aligned(1024))) char smem[PromptLds<T, D>::bytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    PromptTile it;
+    if (!prompt_tile(g, 32, (int)blockIdx.x, lane, it)) return;
+    KeyPlaces<T> keys;
+    keys.in_a_row((const T *)g.k + it.lo * g.ks[0] + it.h * g.ks[1], (const T *)g.v + it.lo * g.vs[0] + it.h * g.vs[1], g.ks[0], g.vs[0]);
+    keys.begin = 0;
+    keys.end = it.row1 - it.lo;
+    const bool live = it.row0 + col < it.row1;
+    const int token = min(it.row0 + col, it.row1 - 1), limit = token - it.lo;
+    const T *q = (const T *)g.q + token * g.qs[0] + it.hq * g.qs[1];
+    f32x16 O[D / 32];
+    float m, s;
+    no_rows_yet(O, m, s);
+    if constexpr (sizeof(T) == 2) {
+        bf16x8 qf[D / 16];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + hf * 8 + ks * 16);
+        narrow_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s, [](int, const f32x16 &) {});
+    } else {
+        float *sQ = (float *)smem;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
+            const int c = wave * (D / 4) + i * 8 + hf * 4;
+            *(f32x4 *)(sQ + col * f32_ld(D) + c) = *(const f32x4 *)(q + c);
+        }
+        __syncthreads();
+        f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, limit, g.c_out, lane, wave, O, m, s, [](int, const f32x16 &) {});
+    }
+    const float *sums = (const float *)(smem + WaveMerge<D>::off_sums);
+    meet_waves<D>(
+        it.row1 - it.row0, live, O, m, s, smem, lane, wave,
+        [&](float M, float all) {
+            if (g.lse) g.lse[(int64_t)it.hq * g.tokens + token] = (M + log2f(all)) * kLn2;
+        },
+        [&](int r, int ch, const f32x4 &o) {
+            store_output((T *)g.out + (it.row0 + r) * g.os[0] + it.hq * g.os[1] + ch, o, 1.f / sums[r]);
+        });
+}
+
+template <class T>
+static hipError_t launch_prompt_t(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
+    if (g.d == 64) hipLaunchKernelGGL((prompt_narrow_kernel<T, 64>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((prompt_narrow_kernel<T, 128>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
+    return hipGetLastError();
+}
+
+hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
+    return g.dtype == AHA_BF16 ? launch_prompt_t<__bf16>(g, pl, st) : launch_prompt_t<float>(g, pl, st);
+}
+
+}  // namespace aha

@@ -1,5 +1,6 @@
 // Entry points of what stands around a prompt's cache: rotation by positions, the paged cache, the attention of a batch
-// that shares prefixes.  All checks run on the host before anything is enqueued.
+// that shares prefixes, of packed prompts, of single tokens over paged caches, and the eviction from these.  All checks run on the host
+// before anything is enqueued.
 #include <math.h>
 
 #include <algorithm>
@@ -174,6 +175,130 @@ static int32_t check_items(const SharedPlan &pl) {
     return AHA_OK;
 }
 
+// Two strides of rows whose head_dim channels are contiguous, as check_stride() has them.
+static int32_t check_pair(const char *name, const int64_t s[2], int dtype, int d, bool out, int64_t n0, int64_t n1) {
+    const int a = 16 / esize(dtype);
+    for (int t = 0; t < 2; ++t) {
+        const int64_t n = t ? n1 : n0;
+        if (s[t] < 0 || s[t] % a != 0)
+            return fail(AHA_ERR_INVALID_ARG, "%s_stride[%d]=%lld must be a non-negative multiple of %d elements", name, t, (long long)s[t], a);
+        if (out && n > 1 && s[t] < d) return fail(AHA_ERR_INVALID_ARG, "%s_stride: rows of what is written would overlap", name);
+    }
+    return AHA_OK;
+}
+static int32_t check_scale(const char *name, float scale) {
+    if (!(scale >= 0.f) || isinf((float)(scale * kLog2e)))
+        return fail(AHA_ERR_INVALID_ARG, "%s must be >= 0 and finite, times log2(e) too", name);
+    return AHA_OK;
+}
+// (never 0, with which a masked logit, -inf, would be no number: a scale of 0 becomes the smallest subnormal, no logit then counts)
+static float log2_scale(float scale) { return std::max((float)(scale * kLog2e), 0x1p-149f); }
+
+static int32_t check_prompt(const aha_prompt *p, bool strides) {
+    if (!p) return fail(AHA_ERR_INVALID_ARG, "params is null");
+    int32_t rc = check_heads(p->sequences, p->tokens, "tokens", p->n_q_heads, p->n_kv_heads, p->head_dim, p->dtype);
+    if (rc) return rc;
+    if (p->n_q_heads % p->n_kv_heads != 0)
+        return fail(AHA_ERR_INVALID_ARG, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
+    if (p->sequences > 65535 || p->n_kv_heads > 65535 || (int64_t)p->tokens * p->n_q_heads > 1 << 30)
+        return fail(AHA_ERR_UNSUPPORTED, "sequences or n_kv_heads exceeds 65535 or tokens * n_q_heads 2^30");
+    if ((rc = check_scale("scale", p->scale))) return rc;
+    if (p->reserved != 0) return fail(AHA_ERR_INVALID_ARG, "reserved must be 0");
+    if (!strides) return AHA_OK;
+    if ((rc = check_pair("q", p->q_stride, p->dtype, p->head_dim, false, 0, 0)) ||
+        (rc = check_pair("k", p->k_stride, p->dtype, p->head_dim, false, 0, 0)) ||
+        (rc = check_pair("v", p->v_stride, p->dtype, p->head_dim, false, 0, 0)))
+        return rc;
+    return check_pair("out", p->out_stride, p->dtype, p->head_dim, true, p->tokens, p->n_q_heads);
+}
+
+static PromptPlan plan_prompt(const aha_prompt *p) {
+    PromptPlan pl{};
+    pl.rows = 32;
+    // every prompt has at most one tile that is not full
+    pl.tiles = ((int64_t)p->tokens + std::min<int64_t>(p->sequences, p->tokens) * (pl.rows - 1)) / pl.rows;
+    pl.items = (pl.tiles * p->n_kv_heads + 7) / 8 * 8 * (p->n_q_heads / p->n_kv_heads);
+    return pl;
+}
+
+// What the attention of single tokens and the eviction have in common.
+static int32_t check_paged(const aha_paged *p, const aha_pages *pg, int q_heads, int least_slots, bool strides) {
+    if (!p) return fail(AHA_ERR_INVALID_ARG, "params is null");
+    if (!pg) return fail(AHA_ERR_INVALID_ARG, "pages is null");
+    int32_t rc = check_heads(p->batch, 1, "batch", q_heads, p->n_kv_heads, p->head_dim, p->dtype);
+    if (rc) return rc;
+    if ((int64_t)p->batch * p->n_kv_heads > 65535) return fail(AHA_ERR_UNSUPPORTED, "batch * n_kv_heads exceeds 65535");
+    if (p->slots < least_slots) return fail(AHA_ERR_INVALID_ARG, "slots (%d) must be >= %d", p->slots, least_slots);
+    if (p->slots > 1 << 30) return fail(AHA_ERR_UNSUPPORTED, "slots beyond 2^30");
+    if (p->budget < 1) return fail(AHA_ERR_INVALID_ARG, "budget (%d) must be >= 1", p->budget);
+    if (p->reserved != 0) return fail(AHA_ERR_INVALID_ARG, "reserved must be 0");
+    return check_pages(pg, p->n_kv_heads, p->dtype, p->head_dim, strides);
+}
+// Rows of `slots` numbers.
+static int32_t check_slots(const char *name, const int64_t s[2], const aha_paged *p, bool out) {
+    const int64_t n[2] = {p->batch, p->n_kv_heads};
+    for (int t = 0; t < 2; ++t) {
+        if (s[t] < 0) return fail(AHA_ERR_INVALID_ARG, "%s_stride[%d] is negative", name, t);
+        if (out && n[t] > 1 && s[t] < p->slots) return fail(AHA_ERR_INVALID_ARG, "%s_stride: rows of what is written would overlap", name);
+    }
+    return AHA_OK;
+}
+
+static int32_t check_paged_attention(const aha_paged *p, const aha_pages *pg, bool strides) {
+    int32_t rc = check_paged(p, pg, p ? p->n_q_heads : 1, 0, strides);
+    if (rc) return rc;
+    if (p->n_q_heads % p->n_kv_heads != 0)
+        return fail(AHA_ERR_INVALID_ARG, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
+    if (p->n_q_heads / p->n_kv_heads > 1024 || (int64_t)p->batch * p->n_q_heads > 1 << 22)
+        return fail(AHA_ERR_UNSUPPORTED, "n_q_heads / n_kv_heads exceeds 1024 or batch * n_q_heads 2^22");
+    if (p->scale_mode != AHA_SCALE_FIXED && p->scale_mode != AHA_SCALE_ADAPTIVE)
+        return fail(AHA_ERR_INVALID_ARG, "scale_mode %d is unknown", p->scale_mode);
+    if ((rc = check_scale("scale", p->scale)) || (rc = check_scale("fixed_scale", p->fixed_scale))) return rc;
+    if (!isfinite((float)(p->lambda_floor * kLog2e))) return fail(AHA_ERR_INVALID_ARG, "lambda_floor must be finite, times log2(e) too");
+    if (!strides) return AHA_OK;
+    if ((rc = check_pair("q", p->q_stride, p->dtype, p->head_dim, false, 0, 0))) return rc;
+    return check_pair("out", p->out_stride, p->dtype, p->head_dim, true, p->batch, p->n_q_heads);
+}
+
+static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
+    PagedPlan pl{};
+    const int group = p->n_q_heads / p->n_kv_heads;
+    const int64_t units = (int64_t)p->batch * p->n_kv_heads;
+    int64_t room = (int64_t)pages->table_width * pages->page_size;
+    if (p->slots > 0) room = std::min<int64_t>(room, p->slots);
+    pl.tiles = (group + 31) / 32;
+    pl.parts = (int)parts_for(units * pl.tiles, room, 32);
+    pl.items = units * pl.tiles * pl.parts;
+    pl.ld = p->slots > 0 ? (room + 31) / 32 * 32 : 0;
+    const size_t rows = (size_t)units * group;
+    pl.off_ms = align_up(sizeof(float) * rows * pl.parts * p->head_dim, 256);
+    pl.off_ms2 = align_up(pl.off_ms + 2 * sizeof(float) * rows * pl.parts, 256);
+    pl.off_dots = align_up(pl.off_ms2 + 2 * sizeof(float) * rows * pl.parts, 256);
+    pl.bytes = align_up(pl.off_dots + sizeof(float) * rows * (size_t)pl.ld, 256);
+    return pl;
+}
+static int32_t check_paged_items(const PagedPlan &pl) {
+    if (pl.items > 1 << 23) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
+    return AHA_OK;
+}
+
+static int32_t check_evict(const aha_paged *p, const aha_pages *pg, bool strides) {
+    const int32_t rc = check_paged(p, pg, 1, 1, strides);
+    if (rc) return rc;
+    if (p->recent < 0 || p->sink < 0 || (int64_t)p->recent + p->sink > p->budget)
+        return fail(AHA_ERR_INVALID_ARG, "recent (%d) and sink (%d) must be >= 0, together at most budget (%d)", p->recent, p->sink, p->budget);
+    return AHA_OK;
+}
+static EvictPlan plan_evict(const aha_paged *p, const aha_pages *pages) {
+    EvictPlan pl{};
+    const int64_t room = std::min<int64_t>((int64_t)pages->table_width * pages->page_size, p->slots);
+    const int64_t units = (int64_t)p->batch * p->n_kv_heads;
+    pl.moves = (int)std::max<int64_t>(0, std::min<int64_t>(p->budget, room - p->budget));
+    pl.off_moves = align_up(sizeof(int32_t) * units, 256);
+    pl.bytes = align_up(pl.off_moves + 2 * sizeof(int32_t) * (size_t)units * pl.moves, 256);
+    return pl;
+}
+
 }  // namespace aha
 
 using namespace aha;
@@ -263,6 +388,113 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
     g.batch = p->batch; g.n = p->q_len; g.Hq = p->n_q_heads; g.Hkv = p->n_kv_heads; g.G = g.Hq / g.Hkv;
     g.d = p->head_dim; g.dtype = p->dtype; g.n_prefixes = p->n_prefixes; g.prefix_cap = p->prefix_cap;
     return hip_result(launch_shared_attention(g, pl, workspace, (hipStream_t)stream), "shared-prefix attention kernels");
+}
+
+int32_t aha_prompt_attention_workspace_bytes(const aha_prompt *p, size_t *out_bytes) {
+    if (!out_bytes) return fail(AHA_ERR_INVALID_ARG, "out_bytes is null");
+    const int32_t rc = check_prompt(p, false);
+    if (rc) return rc;
+    *out_bytes = 0;
+    return AHA_OK;
+}
+
+int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, const void *v, const int32_t *first, void *out, float *lse,
+                             void *workspace, size_t workspace_bytes, void *stream) {
+    int32_t rc = check_prompt(p, true);
+    if (rc) return rc;
+    if ((rc = check_ptr("q", q, 16)) || (rc = check_ptr("k", k, 16)) || (rc = check_ptr("v", v, 16)) || (rc = check_ptr("out", out, 16)) ||
+        (rc = check_ptr("first", first, 4)) || (lse && (rc = check_ptr("lse", lse, 4))))
+        return rc;
+    const PromptPlan pl = plan_prompt(p);
+    // (workgroups of 256 threads: a launch has fewer than 2^32)
+    if (pl.items > 1 << 23) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
+    if ((rc = check_ws(workspace, workspace_bytes, 0))) return rc;
+    PromptGeom g{};
+    g.q = q; g.k = k; g.v = v; g.out = out; g.lse = lse; g.first = first;
+    for (int t = 0; t < 2; ++t) {
+        g.qs[t] = p->q_stride[t]; g.ks[t] = p->k_stride[t]; g.vs[t] = p->v_stride[t]; g.os[t] = p->out_stride[t];
+    }
+    g.tokens = p->tokens; g.sequences = p->sequences; g.Hq = p->n_q_heads; g.Hkv = p->n_kv_heads; g.G = g.Hq / g.Hkv;
+    g.d = p->head_dim; g.dtype = p->dtype; g.c_out = log2_scale(p->scale);
+    return hip_result(launch_prompt_attention(g, pl, (hipStream_t)stream), "prompt attention kernel");
+}
+
+int32_t aha_paged_attention_workspace_bytes(const aha_paged *p, const aha_pages *pages, size_t *out_bytes) {
+    if (!out_bytes) return fail(AHA_ERR_INVALID_ARG, "out_bytes is null");
+    int32_t rc = check_paged_attention(p, pages, false);
+    if (rc) return rc;
+    const PagedPlan pl = plan_paged(p, pages);
+    if ((rc = check_paged_items(pl))) return rc;
+    *out_bytes = pl.bytes;
+    return AHA_OK;
+}
+
+int32_t aha_paged_attention(const aha_paged *p, const aha_pages *pages, const void *q, const void *k_pages, const void *v_pages,
+                            const int32_t *page_table, const int32_t *tail_len, const int32_t *seen, float *scores, int32_t *pos, void *out,
+                            float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    int32_t rc = check_paged_attention(p, pages, true);
+    if (rc) return rc;
+    if ((rc = check_ptr("q", q, 16)) || (rc = check_ptr("k_pages", k_pages, 16)) || (rc = check_ptr("v_pages", v_pages, 16)) ||
+        (rc = check_ptr("page_table", page_table, 4)) || (rc = check_ptr("tail_len", tail_len, 4)) ||
+        (seen && (rc = check_ptr("seen", seen, 4))) || (rc = check_ptr("out", out, 16)) || (lse && (rc = check_ptr("lse", lse, 4))))
+        return rc;
+    if (p->slots == 0 && (scores || pos)) return fail(AHA_ERR_INVALID_ARG, "slots is 0, but scores or pos are given");
+    if (p->slots > 0 && ((rc = check_ptr("scores", scores, 4)) || (rc = check_slots("scores", p->scores_stride, p, true)) ||
+                         (pos && ((rc = check_ptr("pos", pos, 4)) || (rc = check_slots("pos", p->pos_stride, p, true))))))
+        return rc;
+    const PagedPlan pl = plan_paged(p, pages);
+    if ((rc = check_paged_items(pl)) || (rc = check_ws(workspace, workspace_bytes, pl.bytes))) return rc;
+    PagedGeom g{};
+    g.q = q; g.kt = k_pages; g.vt = v_pages; g.out = out; g.lse = lse; g.scores = scores; g.pos = pos; g.seen = seen;
+    for (int t = 0; t < 2; ++t) {
+        g.qs[t] = p->q_stride[t]; g.os[t] = p->out_stride[t]; g.ss[t] = p->scores_stride[t]; g.ps[t] = p->pos_stride[t];
+    }
+    g.pages = page_geom(pages, page_table, tail_len, nullptr);
+    g.batch = p->batch; g.Hq = p->n_q_heads; g.Hkv = p->n_kv_heads; g.G = g.Hq / g.Hkv; g.d = p->head_dim; g.dtype = p->dtype;
+    g.slots = p->slots; g.budget = p->budget; g.scale_mode = p->scale_mode;
+    g.c_out = log2_scale(p->scale); g.fixed_scale = p->fixed_scale; g.lambda_floor = p->lambda_floor;
+    return hip_result(launch_paged_attention(g, pl, workspace, (hipStream_t)stream), "paged attention kernels");
+}
+
+int32_t aha_paged_evict_workspace_bytes(const aha_paged *p, const aha_pages *pages, size_t *out_bytes) {
+    if (!out_bytes) return fail(AHA_ERR_INVALID_ARG, "out_bytes is null");
+    const int32_t rc = check_evict(p, pages, false);
+    if (rc) return rc;
+    *out_bytes = plan_evict(p, pages).bytes;
+    return AHA_OK;
+}
+
+int32_t aha_paged_evict(const aha_paged *p, const aha_pages *pages, const float *scores, const int32_t *pos, void *k_pages, void *v_pages,
+                        const int32_t *page_table, const int32_t *tail_len, const int32_t *seen, float *scores_out, int32_t *pos_out,
+                        int32_t *len_out, void *workspace, size_t workspace_bytes, void *stream) {
+    int32_t rc = check_evict(p, pages, true);
+    if (rc) return rc;
+    if ((rc = check_ptr("scores", scores, 4)) || (pos && (rc = check_ptr("pos", pos, 4))) || (rc = check_ptr("k_pages", k_pages, 16)) ||
+        (rc = check_ptr("v_pages", v_pages, 16)) || (rc = check_ptr("page_table", page_table, 4)) || (rc = check_ptr("tail_len", tail_len, 4)) ||
+        (seen && (rc = check_ptr("seen", seen, 4))) || (rc = check_ptr("scores_out", scores_out, 4)) ||
+        (rc = check_ptr("pos_out", pos_out, 4)) || (rc = check_ptr("len_out", len_out, 4)) ||
+        (rc = check_slots("scores", p->scores_stride, p, false)) || (pos && (rc = check_slots("pos", p->pos_stride, p, false))) ||
+        (rc = check_slots("scores_out", p->scores_out_stride, p, true)) || (rc = check_slots("pos_out", p->pos_out_stride, p, true)))
+        return rc;
+    if (len_out == tail_len) return fail(AHA_ERR_INVALID_ARG, "len_out is tail_len, which other workgroups still read");
+    auto other_rows = [&](const int64_t a[2], const int64_t b[2]) {
+        return (p->batch > 1 && a[0] != b[0]) || (p->n_kv_heads > 1 && a[1] != b[1]);
+    };
+    if ((scores_out == scores && other_rows(p->scores_stride, p->scores_out_stride)) ||
+        (pos_out == pos && other_rows(p->pos_stride, p->pos_out_stride)))
+        return fail(AHA_ERR_INVALID_ARG, "in place, scores and scores_out, or pos and pos_out, must have the same strides");
+    const EvictPlan pl = plan_evict(p, pages);
+    if ((rc = check_ws(workspace, workspace_bytes, pl.bytes))) return rc;
+    EvictGeom g{};
+    g.scores = scores; g.pos = pos; g.seen = seen; g.kt = k_pages; g.vt = v_pages;
+    g.scores_out = scores_out; g.pos_out = pos_out; g.len_out = len_out;
+    for (int t = 0; t < 2; ++t) {
+        g.ss[t] = p->scores_stride[t]; g.ps[t] = p->pos_stride[t]; g.so[t] = p->scores_out_stride[t]; g.po[t] = p->pos_out_stride[t];
+    }
+    g.pages = page_geom(pages, page_table, tail_len, nullptr);
+    g.batch = p->batch; g.Hkv = p->n_kv_heads; g.d = p->head_dim; g.dtype = p->dtype; g.slots = p->slots; g.budget = p->budget;
+    g.recent = p->recent; g.sink = p->sink;
+    return hip_result(launch_paged_evict(g, pl, workspace, (hipStream_t)stream), "eviction kernels");
 }
 
 }  // extern "C"

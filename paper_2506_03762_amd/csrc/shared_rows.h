@@ -8,7 +8,7 @@
 // row's parts.
 #pragma once
 
-#include "score_tile.h"
+#include "key_places.h"
 
 namespace aha {
 
@@ -123,45 +123,17 @@ __device__ __forceinline__ int64_t partial_index(const SharedGeom &g, const Shar
     return ((int64_t)h * (pl.prefix_parts + pl.tail_parts) + part) * g.batch * rows_of_sequence(g) + row;
 }
 
-// Where the key and value rows of an item lie: `entry` is what there is to know of a key beforehand (its page), `at` the rows'
-// offsets in elements from `k` and `v`; what is not there (beyond the end, in a hole) reads as zeros.
-__device__ __attribute__((aligned(256))) const uint32_t kZeroRow[128] = {};
+// The keys of an item.
 template <class T>
-struct SharedKeys {
-    const T *k, *v;
-    int64_t ks, vs;  // tails: of a row in its page; prefixes: of a token
-    int64_t kp, vp;  // tails: of a page
-    const int32_t *table;
-    int shift, pages, begin, end;
-    __device__ __forceinline__ SharedKeys(const SharedGeom &g, const SharedItem &it) : begin(it.begin), end(it.end) {
-        const PageGeom &pg = g.pages;
-        if (it.prefix) {
-            k = (const T *)g.kp + it.which * g.ks[0] + it.h * g.ks[1];
-            v = (const T *)g.vp + it.which * g.vs[0] + it.h * g.vs[1];
-            ks = g.ks[2]; vs = g.vs[2];
-            kp = vp = 0; table = nullptr; shift = 0; pages = 0;
-        } else {
-            k = (const T *)g.kt + it.h * pg.ks[1];
-            v = (const T *)g.vt + it.h * pg.vs[1];
-            ks = pg.ks[2]; vs = pg.vs[2]; kp = pg.ks[0]; vp = pg.vs[0];
-            table = pg.table + (int64_t)it.which * pg.table_width; shift = pg.page_shift; pages = pg.n_pages;
-        }
-    }
-    __device__ __forceinline__ int entry(int key) const { return table ? table[min(key, end - 1) >> shift] : 0; }
-    struct Row {
-        const T *k, *v;
-        bool there;
-    };
-    __device__ __forceinline__ Row at(int key, int page) const {
-        Row r{(const T *)kZeroRow, (const T *)kZeroRow, key < end};
-        if (table) {
-            r.there = r.there && page >= 0 && page < pages;
-            const int row = key & ((1 << shift) - 1);
-            if (r.there) r.k = k + page * kp + row * ks, r.v = v + page * vp + row * vs;
-        } else if (r.there) {
-            r.k = k + key * ks, r.v = v + key * vs;
-        }
-        return r;
+struct SharedKeys : KeyPlaces<T> {
+    __device__ __forceinline__ SharedKeys(const SharedGeom &g, const SharedItem &it) {
+        this->begin = it.begin;
+        this->end = it.end;
+        if (it.prefix)
+            this->in_a_row((const T *)g.kp + it.which * g.ks[0] + it.h * g.ks[1], (const T *)g.vp + it.which * g.vs[0] + it.h * g.vs[1], g.ks[2],
+                           g.vs[2]);
+        else
+            this->in_pages(g.pages, g.kt, g.vt, it.which, it.h);
     }
 };
 
