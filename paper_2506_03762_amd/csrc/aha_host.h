@@ -337,8 +337,13 @@ struct EvictGeom {
     PageGeom pages;
     int batch, Hkv, d, dtype, slots, budget, recent, sink;
 };
+constexpr size_t kEvictStatic = 18 * 1024, kEvictDynamic = 160 * 1024 - kEvictStatic;  // LDS of the selecting workgroup, at most
 struct EvictPlan {
+    int waves;          // of the selecting workgroup
+    int lds_tokens;     // tokens whose keys it holds in LDS
+    size_t lds_bytes;   // of its LDS, beside kEvictStatic
     int moves;          // of a (sequence, KV head), at most
+    bool in_one;        // the selecting workgroup moves keys and values, too
     size_t off_moves, bytes;  // behind the counts: (to, from) of every move
 };
 hipError_t launch_paged_evict(const EvictGeom &g, const EvictPlan &pl, void *ws, hipStream_t st);

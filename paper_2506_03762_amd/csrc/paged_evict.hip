@@ -2,40 +2,69 @@
 // behind the new length move into the places that became free.
 //
 // A token's rank is its key (class and score, order-preserving), its position (the highest goes first) and its place (the last goes first).
-// One workgroup per (sequence, KV head) finds the rank of the last token to go, digit by digit, and lists the moves in order, with
-// scores and positions; a second launch moves keys and values.
+// One workgroup per (sequence, KV head) finds the rank of the last token to go, lists the moves in order and moves scores and positions;
+// it moves the keys and values too where there can only be a few, else a second launch does.
+#include <limits.h>
+
 #include "aha_dev.h"
 #include "aha_host.h"
 
 namespace aha {
 
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
-
 // Ascending order of going: NaN, then scores, then protected tokens.
+constexpr uint32_t kSafe = 0xffffffffu;
 __device__ __forceinline__ uint32_t going_key(float f, bool safe) {
     const uint32_t u = __float_as_uint(f + 0.f);  // (-0 is 0)
-    if (safe) return 0xffffffffu;
-    if (f != f) return 0u;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return safe ? kSafe : f != f ? 0u : key;
 }
 
+// The rank of a token; small ones go.
+struct Rank {
+    uint64_t what;   // key, then the position: the highest first
+    uint32_t place;  // the last first
+    __device__ __forceinline__ bool operator<(const Rank &o) const { return what != o.what ? what < o.what : place < o.place; }
+};
+__device__ __forceinline__ uint64_t rank_what(uint32_t key, int pos) { return (uint64_t)key << 32 | (uint32_t)~((uint32_t)pos ^ 0x80000000u); }
+
+constexpr int kEvictBins = 4096, kEvictCandidates = 1024;
+template <int WAVES>
 struct EvictLds {
-    int hist[256];
-    int wave_count[2][kEvictWaves];
-    int digit, rank;
+    union {
+        int hist[kEvictBins];
+        Rank candidates[kEvictCandidates];
+    };
+    uint32_t all_low, all_above;
+    int all_free;
+    int count[2][WAVES], gaps[WAVES], movers[WAVES];
+    Rank best[WAVES], last;
+    int digit, rank, in_bin, n_candidates;
 };
 
-// The value of rank `rank` (from 0) in ascending order of value(j), j of [0, n) with in(j); `rank` becomes the rank among those of
-// this value.
-template <class In, class Value>
-__device__ __forceinline__ uint32_t value_of_rank(int n, int &rank, EvictLds &sm, In in, Value value) {
+__device__ __forceinline__ int wave_add(int x) {
+    return reduce_lanes<1, 64>(x, [](int a, int b) { return a + b; });
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_prefix(int x, int lane) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int y = __shfl_up(x, s);
+        if (lane >= s) x += y;
+    }
+    return x;
+}
+
+// The value of rank `rank` (from 0) in ascending order of value(j), j of [0, n) with in(j), digit by digit; `rank` becomes the rank among
+// those of this value.
+template <int WAVES, class In, class Value>
+__device__ __forceinline__ uint32_t value_of_rank(int n, int &rank, EvictLds<WAVES> &sm, In in, Value value) {
     const int tid = threadIdx.x;
     uint32_t found = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         __syncthreads();
         if (tid < 256) sm.hist[tid] = 0;
         __syncthreads();
-        for (int j = tid; j < n; j += kEvictThreads)
+        for (int j = tid; j < n; j += WAVES * 64)
             if (in(j)) {
                 const uint32_t x = value(j);
                 if (shift == 24 || (x >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&sm.hist[(x >> shift) & 255], 1);
@@ -45,14 +74,8 @@ __device__ __forceinline__ uint32_t value_of_rank(int n, int &rank, EvictLds &sm
             int c[4], sum = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) c[i] = sm.hist[tid * 4 + i], sum += c[i];
-            int upto = sum;
-#pragma unroll
-            for (int s = 1; s < 64; s *= 2) {
-                const int x = __shfl_up(upto, s);
-                if (tid >= s) upto += x;
-            }
-            int below = upto - sum;
-            if (rank >= below && rank < upto) {
+            int below = wave_prefix(sum, tid) - sum;
+            if (rank >= below && rank < below + sum) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (rank >= below && rank < below + c[i]) sm.digit = tid * 4 + i, sm.rank = rank - below;
@@ -67,109 +90,376 @@ __device__ __forceinline__ uint32_t value_of_rank(int n, int &rank, EvictLds &sm
     return found;
 }
 
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictGeom g, EvictPlan pl, int32_t *counts, int2 *moves) {
-    __shared__ EvictLds sm;
-    const int z = blockIdx.x, b = z / g.Hkv, h = z % g.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t room = min((int64_t)g.pages.table_width << g.pages.page_shift, (int64_t)g.slots);
-    const int len = max(0, (int)min((int64_t)g.pages.tail_len[b], room));
-    const int64_t seen = (g.seen ? g.seen : g.pages.tail_len)[b];
-    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
-    bool hole = false;
-    for (int i = tid; i < (len + (1 << g.pages.page_shift) - 1) >> g.pages.page_shift; i += kEvictThreads)
-        hole |= table[i] < 0 || table[i] >= g.pages.n_pages;
-    const int keep = __syncthreads_or(hole) ? len : min(len, g.budget), go = len - keep;
-    if (h == 0 && tid == 0) g.len_out[b] = keep;
-    const float *scores = g.scores + b * g.ss[0] + h * g.ss[1];
-    const int32_t *pos = g.pos ? g.pos + b * g.ps[0] + h * g.ps[1] : nullptr;
-    float *scores_out = g.scores_out + b * g.so[0] + h * g.so[1];
-    int32_t *pos_out = g.pos_out + b * g.po[0] + h * g.po[1];
-    auto pos_of = [&](int j) { return pos ? pos[j] : j; };
-    auto key_of = [&](int j) {
-        const int p = pos_of(j);
-        return going_key(scores[j], p >= seen - g.recent || p < g.sink);
+// What a workgroup reads of its tokens.
+struct EvictRows {
+    const float *scores;
+    const int32_t *pos;
+    int safe_from, sink;  // positions that are protected: from the one on, before the other
+    __device__ __forceinline__ int pos_of(int j) const { return pos ? pos[j] : j; }
+    __device__ __forceinline__ uint32_t key_of(float score, int p) const { return going_key(score, p >= safe_from || p < sink); }
+    __device__ __forceinline__ uint32_t key_at(int j) const { return key_of(scores[j], pos_of(j)); }
+};
+
+// The last of `go` tokens to go, whatever their scores: key, position and place digit by digit, up to twelve sweeps.
+template <int WAVES>
+__device__ __forceinline__ Rank last_to_go_by_digits(const EvictRows &rows, int len, int go, EvictLds<WAVES> &sm) {
+    auto high_first = [&](int j) { return (uint32_t)rank_what(0, rows.pos_of(j)); };
+    int rank = go - 1;
+    const uint32_t T = value_of_rank(len, rank, sm, [](int) { return true; }, [&](int j) { return rows.key_at(j); });
+    const uint32_t P = value_of_rank(len, rank, sm, [&](int j) { return rows.key_at(j) == T; }, high_first);
+    const uint32_t J = value_of_rank(len, rank, sm, [&](int j) { return rows.key_at(j) == T && high_first(j) == P; }, [](int j) { return ~(uint32_t)j; });
+    return Rank{(uint64_t)T << 32 | P, J};
+}
+
+// Keys and values of moves, in rows of 16-byte chunks.
+__device__ __forceinline__ void move_rows(const EvictGeom &g, const int32_t *table, int h, const int2 *moves, int count, int tid, int threads) {
+    const int esize = g.dtype == AHA_BF16 ? 2 : 4, chunks = g.d * esize / 16, mask = (1 << g.pages.page_shift) - 1;
+    auto row = [&](void *pool, const int64_t s[3], int j, int chunk) {
+        return (u32x4 *)((char *)pool + (table[j >> g.pages.page_shift] * s[0] + h * s[1] + (j & mask) * s[2]) * esize) + chunk;
     };
-    int2 *mine = moves + (int64_t)z * pl.moves;
-    int moved = 0;
-    if (go > 0) {
-        // the last token to go: key T, position P, place J
-        auto high_first = [&](int j) { return ~((uint32_t)pos_of(j) ^ 0x80000000u); };
-        auto last_first = [](int j) { return ~(uint32_t)j; };
-        int rank = go - 1;
-        const uint32_t T = value_of_rank(len, rank, sm, [](int) { return true; }, key_of);
-        const uint32_t P = value_of_rank(len, rank, sm, [&](int j) { return key_of(j) == T; }, high_first);
-        const uint32_t J = value_of_rank(len, rank, sm, [&](int j) { return key_of(j) == T && high_first(j) == P; }, last_first);
-        auto goes = [&](int j) {
-            const uint32_t k = key_of(j);
-            if (k != T) return k < T;
-            const uint32_t p = high_first(j);
-            return p != P ? p < P : last_first(j) <= J;
-        };
-        // free places below `keep` and tokens that stay behind it, both in order
-        int gaps = 0, movers = 0;
-        for (int j0 = 0; j0 < len; j0 += kEvictThreads) {
-            const int j = j0 + tid;
-            const bool there = j < len, gone = there && goes(j), gap = gone && j < keep, mover = there && !gone && j >= keep;
-            const uint64_t gm = __builtin_amdgcn_ballot_w64(gap), mm = __builtin_amdgcn_ballot_w64(mover);
-            __syncthreads();
-            if (lane == 0) sm.wave_count[0][wave] = __builtin_popcountll(gm), sm.wave_count[1][wave] = __builtin_popcountll(mm);
-            __syncthreads();
-            int before[2] = {gaps, movers};
-            for (int w = 0; w < kEvictWaves; ++w) {
-                const int c0 = sm.wave_count[0][w], c1 = sm.wave_count[1][w];
-                if (w < wave) before[0] += c0, before[1] += c1;
-                gaps += c0;
-                movers += c1;
-            }
-            const uint64_t below = ((uint64_t)1 << lane) - 1;
-            if (gap) mine[before[0] + __builtin_popcountll(gm & below)].x = j;
-            if (mover) mine[before[1] + __builtin_popcountll(mm & below)].y = j;
+    constexpr int U = 4;  // rows' chunks in flight
+    for (int i0 = tid; i0 < count * chunks; i0 += U * threads) {
+        u32x4 k[U], v[U];
+        int2 mv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * threads;
+            if (i < count * chunks) mv[u] = moves[i / chunks];
         }
-        moved = gaps;  // (as many as movers)
-        __syncthreads();
-    }
-    if (tid == 0) counts[z] = moved;
-    // every place that keeps its token, where the outputs are others than the inputs (moved ones are written behind the barrier)
-    if (scores_out != scores)
-        for (int j = tid; j < keep; j += kEvictThreads) scores_out[j] = scores[j];
-    if (pos_out != pos)
-        for (int j = tid; j < keep; j += kEvictThreads) pos_out[j] = pos_of(j);
-    __syncthreads();
-    for (int i = tid; i < moved; i += kEvictThreads) {
-        const int2 mv = mine[i];
-        scores_out[mv.x] = scores[mv.y];
-        pos_out[mv.x] = pos_of(mv.y);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * threads;
+            if (i < count * chunks) k[u] = *row(g.kt, g.pages.ks, mv[u].y, i % chunks), v[u] = *row(g.vt, g.pages.vs, mv[u].y, i % chunks);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * threads;
+            if (i < count * chunks) *row(g.kt, g.pages.ks, mv[u].x, i % chunks) = k[u], *row(g.vt, g.pages.vs, mv[u].x, i % chunks) = v[u];
+        }
     }
 }
 
-// Keys and values of the moves: rows of `chunks` 16-byte chunks.
-constexpr int kMoveRows = 16;  // of a workgroup
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictGeom g, EvictPlan pl, int chunks, const int32_t *counts, const int2 *moves) {
-    const int z = blockIdx.y, b = z / g.Hkv, h = z % g.Hkv, count = counts[z], esize = g.dtype == AHA_BF16 ? 2 : 4;
-    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
-    const int mask = (1 << g.pages.page_shift) - 1;
-    for (int i = threadIdx.x; i < kMoveRows * chunks; i += 256) {
-        const int at = blockIdx.x * kMoveRows + i / chunks, c = i % chunks;
-        if (at >= count) return;
-        const int2 mv = moves[(int64_t)z * pl.moves + at];
-        const int to = table[mv.x >> g.pages.page_shift], from = table[mv.y >> g.pages.page_shift];
-        auto move = [&](void *pool, const int64_t s[3]) {
-            auto row = [&](int page, int j) { return (u32x4 *)((char *)pool + (page * s[0] + h * s[1] + (j & mask) * s[2]) * esize) + c; };
-            *row(to, mv.x) = *row(from, mv.y);
-        };
-        move(g.kt, g.pages.ks);
-        move(g.vt, g.pages.vs);
+__device__ __forceinline__ int mask_number(uint64_t m, int from) {  // `from` plus the lanes below this one whose bit is set
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, from));
+}
+// What a workgroup does: `len` tokens, of which `keep` stay.
+struct Eviction {
+    EvictRows rows;
+    float *scores_out;
+    int32_t *pos_out;
+    int2 *moves;
+    int len, keep;
+    // token `from` goes to place `to`
+    __device__ __forceinline__ void move(int i, int to, int from) const {
+        moves[i] = make_int2(to, from);
+        scores_out[to] = rows.scores[from];
+        pos_out[to] = rows.pos_of(from);
     }
+    // every place that keeps its token, where the outputs are others than the inputs (places that get another one are written behind a
+    // barrier)
+    __device__ __forceinline__ void copy(int tid, int threads) const {
+        const bool s = scores_out != rows.scores, p = pos_out != rows.pos;
+        if (!s && !p) return;
+        for (int j = tid; j < keep; j += 4 * threads) {
+            float x[4];
+            int y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = rows.scores[min(j + u * threads, keep - 1)], y[u] = rows.pos_of(min(j + u * threads, keep - 1));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j + u * threads < keep) {
+                    if (s) scores_out[j + u * threads] = x[u];
+                    if (p) pos_out[j + u * threads] = y[u];
+                }
+        }
+    }
+};
+
+// The tokens' keys in LDS, `steps` steps of 64 tokens of a wave, one lane each, which alone reads them.  Returns the number of moves.
+// (`holes`: all threads call it; whether the sequence has one)
+template <int WAVES, class Holes>
+__device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, uint32_t *keys, uint16_t *gap_places, int tid, Holes holes) {
+    constexpr int THREADS = WAVES * 64, U = WAVES == 16 ? 32 : 8;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), len = e.len;
+    const int per_wave = (len + THREADS - 1) / THREADS * 64, first = wave * per_wave, steps = min(per_wave, max(0, len - first) + 63) / 64;
+    const int base = first + lane;
+    const EvictRows &rows = e.rows;
+    uint32_t *key = keys + base;
+    if (tid == 0) sm.all_low = kSafe, sm.all_above = 0, sm.all_free = 0, sm.n_candidates = 0;
+    // the range of the keys that may go, and their number
+    uint32_t low = kSafe, above = 0;
+    int free_keys = 0;
+    for (int t0 = 0; t0 < steps; t0 += U) {  // (U steps' scores and positions are requested before any is used)
+        float score[U];
+        int pos[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t0 + u < steps) {
+                const int j = min(base + (t0 + u) * 64, len - 1);
+                score[u] = rows.scores[j];
+                pos[u] = rows.pos_of(j);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t0 + u < steps) {
+                uint32_t k = rows.key_of(score[u], pos[u]);
+                if (base + (t0 + u) * 64 >= len) k = kSafe;  // (counts as a protected one; `rank_of` is asked of tokens alone)
+                key[(t0 + u) * 64] = k;
+                low = min(low, k);
+                above = max(above, k + 1);  // (0 of protected ones)
+                free_keys += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k != kSafe));
+            }
+    }
+    if (holes()) {  // (behind a barrier)
+        e.keep = len;
+        return 0;
+    }
+    const int keep = e.keep, go = len - keep;
+    auto rank_of = [&](int t, uint32_t k) { return Rank{rank_what(k, rows.pos_of(base + t * 64)), ~(uint32_t)(base + t * 64)}; };
+    low = reduce_lanes<1, 64>(low, OpMinU{});
+    above = reduce_lanes<1, 64>(above, OpMaxU{});
+    if (lane == 0) atomicMin(&sm.all_low, low), atomicMax(&sm.all_above, above), atomicAdd(&sm.all_free, free_keys);
+    if (go > 1)
+        for (int i = tid; i < kEvictBins; i += THREADS) sm.hist[i] = 0;
+    __syncthreads();
+    low = sm.all_low;
+    above = sm.all_above;
+    free_keys = sm.all_free;
+    Rank last;
+    if (go == 1) {  // the smallest
+        Rank best{~(uint64_t)0, ~0u};
+        bool any = false;
+        for (int t = 0; t < steps; ++t)
+            if (key[t * 64] == low && base + t * 64 < len) {
+                const Rank r = rank_of(t, low);
+                if (r < best) best = r;
+                any = true;
+            }
+        if (__builtin_amdgcn_ballot_w64(any)) {
+#pragma unroll
+            for (int s = 32; s > 0; s /= 2) {
+                const Rank r{__shfl_xor((unsigned long long)best.what, s), (uint32_t)__shfl_xor((int)best.place, s)};
+                if (r < best) best = r;
+            }
+        }
+        if (lane == 0) sm.best[wave] = best;
+        __syncthreads();
+        last = sm.best[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+            if (sm.best[w] < last) last = sm.best[w];
+        const int gone = (int)~last.place;
+        if (gone >= keep) return 0;  // (the last token itself)
+        if (tid == 0) e.move(0, gone, keep);
+        return 1;
+    }
+    bool found = false;
+    if (go <= free_keys) {
+        // one histogram, linear over that range; the bin of the last one to go; its keys ranked against each other
+        const uint32_t range = above - 1 - low;
+        const uint32_t slope = range < kEvictBins ? 0u : (uint32_t)(((uint64_t)kEvictBins << 32) / ((uint64_t)range + 1));
+        auto bin_of = [&](uint32_t k) { return (int)(slope ? __umulhi(k - low, slope) : k - low); };
+#pragma unroll 4
+        for (int t = 0; t < steps; ++t) {
+            const uint32_t k = key[t * 64];
+            if (k != kSafe) atomicAdd(&sm.hist[bin_of(k)], 1);
+        }
+        __syncthreads();
+        constexpr int BPT = kEvictBins / THREADS;
+        int c[BPT], sum = 0;
+#pragma unroll
+        for (int i = 0; i < BPT; ++i) c[i] = sm.hist[tid * BPT + i], sum += c[i];
+        int below = wave_prefix(sum, lane);
+        if (lane == 63) sm.count[1][wave] = below;
+        __syncthreads();
+        below -= sum;
+        for (int w = 0; w < wave; ++w) below += sm.count[1][w];
+        if (go > below && go <= below + sum) {
+#pragma unroll
+            for (int i = 0; i < BPT; ++i) {
+                if (go > below && go <= below + c[i]) sm.digit = tid * BPT + i, sm.rank = go - 1 - below, sm.in_bin = c[i];
+                below += c[i];
+            }
+        }
+        __syncthreads();
+        const int bin = sm.digit, in_bin = sm.in_bin, want = sm.rank;
+        if (in_bin <= kEvictCandidates) {
+            found = true;
+#pragma unroll 4
+            for (int t = 0; t < steps; ++t) {
+                const uint32_t k = key[t * 64];
+                if (k != kSafe && bin_of(k) == bin) sm.candidates[atomicAdd(&sm.n_candidates, 1)] = rank_of(t, k);
+            }
+            __syncthreads();
+            for (int i = tid; i < in_bin; i += THREADS) {
+                const Rank r = sm.candidates[i];
+                int smaller = 0;
+                for (int o = 0; o < in_bin; ++o) smaller += sm.candidates[o] < r;
+                if (smaller == want) sm.last = r;
+            }
+            __syncthreads();
+            last = sm.last;
+        }
+    }
+    // what goes now has keys up to `last_key`, what stays larger ones
+    uint32_t last_key;
+    if (found) {
+        last_key = (uint32_t)(last.what >> 32);
+        for (int i = tid; i < sm.in_bin; i += THREADS) {
+            const Rank r = sm.candidates[i];
+            if ((uint32_t)(r.what >> 32) == last_key && last < r) keys[~r.place] = kSafe;
+        }
+        __syncthreads();
+    } else {
+        last = last_to_go_by_digits(rows, len, go, sm);
+        last_key = 0;
+        for (int t = 0; t < steps; ++t)
+            if (base + t * 64 < len) key[t * 64] = last < rank_of(t, key[t * 64]) ? kSafe : 0u;
+    }
+    // free places below `keep` and tokens that stay behind it, both in order
+    const int front_steps = min(steps, max(0, keep - first + 63) / 64), back = min(steps, max(0, keep - first) / 64);  // steps with places below
+                                                                                                                        // `keep`, the first one with others
+    auto is_gap = [&](int t) { return key[t * 64] <= last_key && base + t * 64 < keep; };
+    auto is_mover = [&](int t) { return key[t * 64] > last_key && (uint32_t)(base + t * 64 - keep) < (uint32_t)go; };
+    int gaps = 0, movers = 0;
+#pragma unroll 8
+    for (int t = 0; t < front_steps; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is_gap(t)));
+#pragma unroll 8
+    for (int t = back; t < steps; ++t) movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is_mover(t)));
+    if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
+    __syncthreads();
+    gaps = movers = 0;
+    int moved = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        moved += sm.gaps[w];  // (as many as movers)
+        if (w < wave) gaps += sm.gaps[w], movers += sm.movers[w];
+    }
+    gaps = __builtin_amdgcn_readfirstlane(gaps);
+    movers = __builtin_amdgcn_readfirstlane(movers);
+    uint16_t *mover_places = gap_places + moved;
+#pragma unroll 8
+    for (int t = 0; t < front_steps; ++t) {
+        const bool gap = is_gap(t);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(gap);
+        if (gap) gap_places[mask_number(m, gaps)] = (uint16_t)(base + t * 64);
+        gaps += __builtin_popcountll(m);
+    }
+#pragma unroll 8
+    for (int t = back; t < steps; ++t) {
+        const bool mover = is_mover(t);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(mover);
+        if (mover) mover_places[mask_number(m, movers)] = (uint16_t)(base + t * 64);
+        movers += __builtin_popcountll(m);
+    }
+    __syncthreads();
+    for (int i = tid; i < moved; i += THREADS) e.move(i, gap_places[i], mover_places[i]);
+    return moved;
+}
+
+// More tokens than that: keys are read again whenever they are needed.
+template <int WAVES>
+__device__ __forceinline__ int evict_from_memory(const Eviction &e, EvictLds<WAVES> &sm, int tid) {
+    constexpr int THREADS = WAVES * 64;
+    const int lane = tid & 63, wave = tid >> 6, len = e.len, keep = e.keep;
+    const EvictRows &rows = e.rows;
+    const Rank last = last_to_go_by_digits(rows, len, len - keep, sm);
+    int gaps = 0, movers = 0;
+    for (int j0 = 0; j0 < len; j0 += THREADS) {
+        const int j = j0 + tid;
+        const bool there = j < len, goes = there && !(last < Rank{rank_what(rows.key_at(min(j, len - 1)), rows.pos_of(min(j, len - 1))), ~(uint32_t)j});
+        const bool gap = goes && j < keep, mover = there && !goes && j >= keep;
+        const uint64_t gm = __builtin_amdgcn_ballot_w64(gap), mm = __builtin_amdgcn_ballot_w64(mover);
+        __syncthreads();
+        if (lane == 0) sm.count[0][wave] = __builtin_popcountll(gm), sm.count[1][wave] = __builtin_popcountll(mm);
+        __syncthreads();
+        int before[2] = {gaps, movers};
+        for (int w = 0; w < WAVES; ++w) {
+            const int c0 = sm.count[0][w], c1 = sm.count[1][w];
+            if (w < wave) before[0] += c0, before[1] += c1;
+            gaps += c0;
+            movers += c1;
+        }
+        if (gap) e.moves[mask_number(gm, before[0])].x = j;
+        if (mover) e.moves[mask_number(mm, before[1])].y = j;
+    }
+    __syncthreads();
+    for (int i = tid; i < gaps; i += THREADS) {
+        const int2 mv = e.moves[i];
+        e.move(i, mv.x, mv.y);
+    }
+    return gaps;  // (as many as movers)
+}
+
+// Dynamic LDS: the keys of pl.lds_tokens tokens (and of the places behind the last), then the places that become free and those that
+// move.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictGeom g, EvictPlan pl, int32_t *counts, int2 *moves) {
+    constexpr int THREADS = WAVES * 64;
+    __shared__ EvictLds<WAVES> sm;
+    extern __shared__ __attribute__((aligned(16))) uint32_t dynamic[];
+    const int z = blockIdx.x, b = z / g.Hkv, h = z % g.Hkv, tid = threadIdx.x;
+    const int64_t room = min((int64_t)g.pages.table_width << g.pages.page_shift, (int64_t)g.slots);
+    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
+    Eviction e;
+    e.len = __builtin_amdgcn_readfirstlane(max(0, (int)min((int64_t)g.pages.tail_len[b], room)));
+    e.keep = min(e.len, g.budget);
+    e.rows = EvictRows{g.scores + b * g.ss[0] + h * g.ss[1], g.pos ? g.pos + b * g.ps[0] + h * g.ps[1] : nullptr,
+                       (int)max((int64_t)(g.seen ? g.seen : g.pages.tail_len)[b] - g.recent, (int64_t)INT_MIN), g.sink};
+    e.scores_out = g.scores_out + b * g.so[0] + h * g.so[1];
+    e.pos_out = g.pos_out + b * g.po[0] + h * g.po[1];
+    e.moves = moves + (int64_t)z * pl.moves;
+    auto holes = [&] {
+        bool hole = false;
+        const int pages = (int)(((int64_t)e.len + (1 << g.pages.page_shift) - 1) >> g.pages.page_shift);
+        for (int i = tid; i < pages; i += THREADS) hole |= table[i] < 0 || table[i] >= g.pages.n_pages;
+        e.copy(tid, THREADS);
+        return __syncthreads_or(hole) != 0;
+    };
+    static_assert(sizeof(sm) <= kEvictStatic, "what the plan leaves for it");
+    int moved = 0;
+    if (e.len == e.keep) {
+        e.copy(tid, THREADS);
+    } else if (e.len <= pl.lds_tokens) {
+        moved = evict_in_lds<WAVES>(e, sm, dynamic, (uint16_t *)(dynamic + (pl.lds_tokens + THREADS)), tid, holes);
+    } else if (holes()) {
+        e.keep = e.len;
+    } else {
+        moved = evict_from_memory(e, sm, tid);
+    }
+    if (e.keep > g.budget) e.copy(tid, THREADS);  // (a hole: all places)
+    if (tid == 0) {
+        counts[z] = moved;
+        if (h == 0) g.len_out[b] = e.keep;
+    }
+    if (pl.in_one) {
+        __syncthreads();
+        move_rows(g, table, h, e.moves, moved, tid, THREADS);
+    }
+}
+
+constexpr int kMoveRows = 16;  // of a workgroup
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictGeom g, EvictPlan pl, const int32_t *counts, const int2 *moves) {
+    const int z = blockIdx.y, b = z / g.Hkv, first = blockIdx.x * kMoveRows;
+    const int count = min(kMoveRows, counts[z] - first);
+    move_rows(g, g.pages.table + (int64_t)b * g.pages.table_width, z % g.Hkv, moves + (int64_t)z * pl.moves + first, count, threadIdx.x, 256);
 }
 
 hipError_t launch_paged_evict(const EvictGeom &g, const EvictPlan &pl, void *ws, hipStream_t st) {
     int32_t *counts = (int32_t *)ws;
     int2 *moves = (int2 *)((char *)ws + pl.off_moves);
     const int Z = g.batch * g.Hkv;
-    hipLaunchKernelGGL(evict_select_kernel, dim3(Z), dim3(kEvictThreads), 0, st, g, pl, counts, moves);
+    static DeviceOnce once;
+    const hipError_t e0 = device_once(once, [] {
+        return hipFuncSetAttribute((const void *)evict_select_kernel<16>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kEvictDynamic);
+    });
+    if (e0 != hipSuccess) return e0;
+    auto select = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3(Z), dim3(waves * 64), pl.lds_bytes, st, g, pl, counts, moves); };
+    if (pl.waves == 4) select(evict_select_kernel<4>, 4);
+    else if (pl.waves == 8) select(evict_select_kernel<8>, 8);
+    else select(evict_select_kernel<16>, 16);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pl.moves == 0) return e;
-    const int chunks = g.d * (g.dtype == AHA_BF16 ? 2 : 4) / 16;
-    hipLaunchKernelGGL(evict_move_kernel, dim3((pl.moves + kMoveRows - 1) / kMoveRows, Z), dim3(256), 0, st, g, pl, chunks, counts, moves);
+    if (e != hipSuccess || pl.moves == 0 || pl.in_one) return e;
+    hipLaunchKernelGGL(evict_move_kernel, dim3((pl.moves + kMoveRows - 1) / kMoveRows, Z), dim3(256), 0, st, g, pl, counts, moves);
     return hipGetLastError();
 }
 

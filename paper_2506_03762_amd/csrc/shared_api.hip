@@ -294,6 +294,13 @@ static EvictPlan plan_evict(const aha_paged *p, const aha_pages *pages) {
     const int64_t room = std::min<int64_t>((int64_t)pages->table_width * pages->page_size, p->slots);
     const int64_t units = (int64_t)p->batch * p->n_kv_heads;
     pl.moves = (int)std::max<int64_t>(0, std::min<int64_t>(p->budget, room - p->budget));
+    // keys of as many tokens as there can be or as fit, of the places that fill the last step of every wave, and 16 bits for each place that
+    // becomes free (as many as tokens lie behind it, at most) and each that moves
+    pl.waves = room <= 1024 ? 4 : room <= 4096 ? 8 : 16;
+    const int64_t words = (int64_t)kEvictDynamic / 4 - 64 * pl.waves - 4;
+    pl.lds_tokens = (int)std::min<int64_t>(room, std::max<int64_t>(words - pl.moves, words * 2 / 3));
+    pl.lds_bytes = align_up(4 * ((size_t)pl.lds_tokens + 64 * pl.waves + std::min(pl.moves, pl.lds_tokens / 2)), 16);
+    pl.in_one = pl.moves <= 256;
     pl.off_moves = align_up(sizeof(int32_t) * units, 256);
     pl.bytes = align_up(pl.off_moves + 2 * sizeof(int32_t) * (size_t)units * pl.moves, 256);
     return pl;
