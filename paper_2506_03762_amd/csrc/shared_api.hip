@@ -2,6 +2,7 @@
 // that shares prefixes, of packed prompts, of single tokens over paged caches, and the eviction from these.  All checks run on the host
 // before anything is enqueued.
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -214,10 +215,15 @@ static int32_t check_prompt(const aha_prompt *p, bool strides) {
 
 static PromptPlan plan_prompt(const aha_prompt *p) {
     PromptPlan pl{};
-    pl.rows = 32;
-    // every prompt has at most one tile that is not full
-    pl.tiles = ((int64_t)p->tokens + std::min<int64_t>(p->sequences, p->tokens) * (pl.rows - 1)) / pl.rows;
-    pl.items = (pl.tiles * p->n_kv_heads + 7) / 8 * 8 * (p->n_q_heads / p->n_kv_heads);
+    const char *force = getenv("AHA_PROMPT_ROWS");
+    pl.rows = p->dtype != AHA_BF16 ? 32 : force ? atoi(force) : 256;
+    const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads;
+    if (pl.rows > 32) {  // at most one block of 64 rows, and one tile, of every prompt that is not full
+        const int64_t blocks = (p->tokens + 63 * prompts) / 64;
+        pl.items = (blocks * group + prompts * 3) / 4 * p->n_kv_heads;
+    } else {
+        pl.items = ((p->tokens + 31 * prompts) / 32 * p->n_kv_heads + 7) / 8 * 8 * group;
+    }
     return pl;
 }
 
