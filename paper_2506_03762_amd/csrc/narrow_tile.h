@@ -154,14 +154,40 @@ __device__ __forceinline__ void f32_sweep(const Keys &keys, const float *sq, int
     using A = NarrowRows<D>;
     constexpr int CB = D / 32;
     const int col = lane & 31, hf = lane >> 5, limit_min = -reduce_lanes<1, 32>(-limit, OpMaxI{});
-    for (int kb = keys.begin + wave * 32; kb < keys.end; kb += A::STEP) {
-        const auto here = keys.at(kb + col, keys.entry(kb + col));
-        const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(here.there);
-        f32x4 a[D / 8];
+    int kb = keys.begin + wave * 32;
+    if (kb >= keys.end) return;
+    // a block's values are requested in front of its dots, the next one's keys behind them, its page a block earlier
+    int next_entry = keys.entry(kb + A::STEP + col);
+    auto here = keys.at(kb + col, keys.entry(kb + col));
+    f32x4 a[D / 8];
+    auto load_keys = [&] {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) a[i] = *(const f32x4 *)(here.k + 4 * hf + 8 * i);
+    };
+    load_keys();
+    for (; kb < keys.end; kb += A::STEP) {
+        const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(here.there);
+        float v_row[16][CB];
+        const uint64_t mine = (uint64_t)(uintptr_t)here.v;
+        auto load_values = [&](int v) {
+            const int from = 8 * (v >> 2) + 4 * hf + (v & 3);
+            const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
+            const float *vr = (const float *)(((uint64_t)hi << 32) | lo) + col;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) v_row[v][cb] = vr[cb * 32];
+        };
+        constexpr int AHEAD = D == 64 ? 16 : 0;  // (d = 128: they do not fit beside the dots' chains)
+#pragma unroll
+        for (int v = 0; v < AHEAD; ++v) load_values(v);
+        here = keys.at(kb + A::STEP + col, next_entry);
+        next_entry = keys.entry(kb + 2 * A::STEP + col);
+        __builtin_amdgcn_sched_barrier(0);
         f32x16 acc = dots_f32<D>(a, sq);
-        __builtin_amdgcn_sched_barrier(0);  // (value rows requested in front of the products take the registers of the chains)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int v = AHEAD; v < 16; ++v) load_values(v);
+        load_keys();
+        __builtin_amdgcn_sched_barrier(0);
         if (there != 0xffffffffu || kb + 31 > limit_min) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
@@ -189,15 +215,10 @@ __device__ __forceinline__ void f32_sweep(const Keys &keys, const float *sq, int
         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
-        const uint64_t mine = (uint64_t)(uintptr_t)here.v;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int from = 8 * (v >> 2) + 4 * hf + (v & 3);
-            const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
-            const float *vr = (const float *)(((uint64_t)hi << 32) | lo) + col;
+        for (int v = 0; v < 16; ++v)
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) O[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[cb * 32], acc[v], O[cb], 0, 0, 0);
-        }
+            for (int cb = 0; cb < CB; ++cb) O[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_row[v][cb], acc[v], O[cb], 0, 0, 0);
     }
 }
 

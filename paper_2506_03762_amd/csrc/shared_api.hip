@@ -2,7 +2,6 @@
 // that shares prefixes, of packed prompts, of single tokens over paged caches, and the eviction from these.  All checks run on the host
 // before anything is enqueued.
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -215,9 +214,13 @@ static int32_t check_prompt(const aha_prompt *p, bool strides) {
 
 static PromptPlan plan_prompt(const aha_prompt *p) {
     PromptPlan pl{};
-    const char *force = getenv("AHA_PROMPT_ROWS");
-    pl.rows = p->dtype != AHA_BF16 ? 32 : force ? atoi(force) : 256;
     const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads;
+    // Tiles of 256 rows where they fill a good part of the chip, by a count as if prompts ended evenly in their last block of 64 rows.  us in tiles of 32 and
+    // of 256 rows, d = 128, 4 query heads of each KV head: 8 heads, prompts of 512 tokens 15.7, 21.9, 768 27.7, 28.6, 1024 36.0, 34.9, 2048 95.0, 62.0,
+    // 16 of 64 16.8, 11.1, 4 of 200 18.9, 14.4; 2 heads, one of 2048 36.9, 59.4, 4 of 500 17.6, 21.8, 16 of 200 21.1, 15.0; d = 64, 16 of 16 heads,
+    // one of 2048 32.2, 48.1, 4 of 500 17.1, 19.1, 16 of 200 22.4, 13.4; 6 of 2 heads, 16 of 200 12.0, 12.0, of 500 26.0, 19.0.
+    const int64_t even = ((int64_t)p->tokens + 31 * prompts) / 64 * group * p->n_kv_heads;
+    pl.rows = p->dtype == AHA_BF16 && even / 4 >= (p->head_dim == 64 ? 176 : 112) ? 256 : 32;
     if (pl.rows > 32) {  // at most one block of 64 rows, and one tile, of every prompt that is not full
         const int64_t blocks = (p->tokens + 63 * prompts) / 64;
         pl.items = (blocks * group + prompts * 3) / 4 * p->n_kv_heads;
