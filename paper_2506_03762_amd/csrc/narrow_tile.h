@@ -30,9 +30,10 @@ __device__ __forceinline__ void no_rows_yet(f32x16 (&O)[CB], float &m, float &s)
 #pragma unroll
         for (int v = 0; v < 16; ++v) O[cb][v] = 0.f;
 }
-// `limit`: the last key that the lane's row sees.  `block(kb, acc)` is told the products of the 32 keys from kb on, those that a row does
+// ONCE: the values are read past the caches, as no other tile reads them (64 caches of up to 4096 tokens, 8 heads of 128 160 us, so 156; the keys too
+// 191: a lane's pieces of a row come with eight loads, which then read it again).  `limit`: the last key that the lane's row sees.  `block(kb, acc)` is told the products of the 32 keys from kb on, those that a row does
 // not see -inf.
-template <int D, class Keys, class Block>
+template <int D, bool ONCE = false, class Keys, class Block>
 __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf)[D / 16], int limit, float c_out, char *smem, int lane, int wave,
                                              f32x16 (&O)[D / 32], float &m, float &s, Block block) {
     using A = NarrowRows<D>;
@@ -48,10 +49,16 @@ __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf
             const int from = j * A::RPI + lr;
             const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
             const uint64_t src = (((uint64_t)hi << 32) | lo) + chunk * 16;
-            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                         :
-                         : "v"(src), "s"(lds0 + buf * (int)A::v_bytes + j * 1024)
-                         : "memory");
+            if constexpr (ONCE)
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
+                             :
+                             : "v"(src), "s"(lds0 + buf * (int)A::v_bytes + j * 1024)
+                             : "memory");
+            else
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                             :
+                             : "v"(src), "s"(lds0 + buf * (int)A::v_bytes + j * 1024)
+                             : "memory");
         }
     };
     bf16x8 a[KS];

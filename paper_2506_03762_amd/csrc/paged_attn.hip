@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, 2) void paged_part_kernel(PagedGeom g, PagedPl
             qf[ks] = *(const bf16x8 *)(q + hf * 8 + ks * 16);
             if (!live) qf[ks] = bf16x8{};
         }
-        narrow_sweep<D>(keys, qf, INT_MAX, g.c_out, smem, lane, wave, O, m, s, block);
+        narrow_sweep<D, true>(keys, qf, INT_MAX, g.c_out, smem, lane, wave, O, m, s, block);
     } else {
         float *sQ = (float *)smem;
 #pragma unroll
@@ -167,11 +167,26 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedGeom g, PagedPlan 
         if (g.lse && ch == 0) g.lse[(int64_t)b * g.Hq + hq] = x.s == 0.f ? -INFINITY : (x.m + log2f(x.s)) * kLn2;
         return;
     }
-    // ---- scores ----
-    const int len = tokens_of(g, b), k0 = (blockIdx.x - out_wgs) * kJoinKeys;
-    if (k0 >= len) return;
+    // ---- scores: a thread takes four tokens ----
+    // (the products of the first rows, scores and pages are requested before anything of the sequence is known: they lie within the
+    // workspace's rows, the table and scores wherever its end is)
     __shared__ float2 norm[kMaxGroup];  // of every row: reference, 1 / sum
-    const int lane = tid & 63;
+    const int lane = tid & 63, j0 = (blockIdx.x - out_wgs) * kJoinKeys + 4 * tid, at = min(j0, (int)pl.ld - 4);
+    const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld + at;
+    float *F = g.scores + b * g.ss[0] + h * g.ss[1];
+    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
+    f32x4 dot[U];
+    float score[4];
+    int page[4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) dot[u] = *(const f32x4 *)(x + min(u, g.G - 1) * pl.ld);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        score[i] = F[min(at + i, g.slots - 1)];
+        page[i] = table[min((at + i) >> g.pages.page_shift, g.pages.table_width - 1)];
+    }
+    const int len = tokens_of(g, b), seen = (g.seen ? g.seen : g.pages.tail_len)[b];
+    if ((blockIdx.x - out_wgs) * kJoinKeys >= len) return;
     for (int gi = tid >> 6; gi < g.G; gi += 4) {  // (up to 64 parts, one per lane)
         const float2 ms = lane < pl.parts ? part_ms2[paged_partial(g, pl, z, lane, gi)] : make_float2(-INFINITY, 0.f);
         const float M = wave_max(ms.x), ref = M == -INFINITY ? 0.f : M, all = wave_sum(fast_exp2(ms.x - ref) * ms.y);
@@ -179,17 +194,31 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedGeom g, PagedPlan 
     }
     __syncthreads();
     const float lam = score_scale(g, b);
-    const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld;
-    float *F = g.scores + b * g.ss[0] + h * g.ss[1];
-    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
-    for (int j = k0 + tid; j < min(len, k0 + kJoinKeys); j += 256) {
-        float w = 0.f;
-        for (int gi = 0; gi < g.G; ++gi) w += fast_exp2(fmaf(x[gi * pl.ld + j], lam, -norm[gi].x)) * norm[gi].y;
-        const int page = table[j >> g.pages.page_shift];
-        const bool there = page >= 0 && page < g.pages.n_pages;
-        if (j == len - 1) F[j] = there ? w : 0.f;
-        else if (there) F[j] += w;
-        if (j == len - 1 && g.pos) g.pos[b * g.ps[0] + h * g.ps[1] + j] = (g.seen ? g.seen : g.pages.tail_len)[b] - 1;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < g.G; g0 += U) {
+        if (g0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) dot[u] = *(const f32x4 *)(x + min(g0 + u, g.G - 1) * pl.ld);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (g0 + u < g.G) {
+                const float2 n = norm[g0 + u];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] += fast_exp2(fmaf(dot[u][i], lam, -n.x)) * n.y;
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + i;
+        if (j >= len) break;
+        const bool there = page[i] >= 0 && page[i] < g.pages.n_pages;
+        if (j == len - 1) {
+            F[j] = there ? w[i] : 0.f;
+            if (g.pos) g.pos[b * g.ps[0] + h * g.ps[1] + j] = seen - 1;
+        } else if (there) {
+            F[j] = score[i] + w[i];
+        }
     }
 }
 

@@ -276,7 +276,9 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     int64_t room = (int64_t)pages->table_width * pages->page_size;
     if (p->slots > 0) room = std::min<int64_t>(room, p->slots);
     pl.tiles = (group + 31) / 32;
-    pl.parts = (int)parts_for(units * pl.tiles, room, 32);
+    // (no part of more than 1024 places: sequences' lengths differ.  64 of up to 4096 tokens, 8 heads: 168 us with one part each, 160 with four, 167 with
+    // eight)
+    pl.parts = (int)std::max(parts_for(units * pl.tiles, room, 32), std::min<int64_t>(64, room / 1024));
     pl.items = units * pl.tiles * pl.parts;
     pl.ld = p->slots > 0 ? (room + 31) / 32 * 32 : 0;
     const size_t rows = (size_t)units * group;
