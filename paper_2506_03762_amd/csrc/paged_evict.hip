@@ -6,6 +6,8 @@
 // it moves the keys and values too where there can only be a few, else a second launch does.
 #include <limits.h>
 
+#include <type_traits>
+
 #include "aha_dev.h"
 #include "aha_host.h"
 
@@ -34,7 +36,7 @@ struct EvictLds {
         int hist[kEvictBins];
         Rank candidates[kEvictCandidates];
     };
-    uint32_t all_low, all_above;
+    uint32_t all_low, all_above, from, to;
     int all_free;
     int count[2][WAVES], gaps[WAVES], movers[WAVES];
     Rank best[WAVES], last;
@@ -96,7 +98,8 @@ struct EvictRows {
     const int32_t *pos;
     int safe_from, sink;  // positions that are protected: from the one on, before the other
     __device__ __forceinline__ int pos_of(int j) const { return pos ? pos[j] : j; }
-    __device__ __forceinline__ uint32_t key_of(float score, int p) const { return going_key(score, p >= safe_from || p < sink); }
+    __device__ __forceinline__ bool safe(int p) const { return p >= safe_from || p < sink; }
+    __device__ __forceinline__ uint32_t key_of(float score, int p) const { return going_key(score, safe(p)); }
     __device__ __forceinline__ uint32_t key_at(int j) const { return key_of(scores[j], pos_of(j)); }
 };
 
@@ -179,7 +182,7 @@ struct Eviction {
 // (`holes`: all threads call it; whether the sequence has one)
 template <int WAVES, class Holes>
 __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, uint32_t *keys, uint16_t *gap_places, int tid, Holes holes) {
-    constexpr int THREADS = WAVES * 64, U = WAVES == 16 ? 32 : 8;
+    constexpr int THREADS = WAVES * 64, U = WAVES == 16 ? 16 : 4;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), len = e.len;
     const int per_wave = (len + THREADS - 1) / THREADS * 64, first = wave * per_wave, steps = min(per_wave, max(0, len - first) + 63) / 64;
     const int base = first + lane;
@@ -189,26 +192,56 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     // the range of the keys that may go, and their number
     uint32_t low = kSafe, above = 0;
     int free_keys = 0;
-    for (int t0 = 0; t0 < steps; t0 += U) {  // (U steps' scores and positions are requested before any is used)
-        float score[U];
+    auto count = [&](uint32_t k) {
+        low = min(low, k);
+        above = max(above, k + 1);  // (0 of protected ones)
+        free_keys += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k != kSafe));
+    };
+    // U steps' scores and positions are requested before any is used; WHOLE: all U of them, and no place behind the last token (with 32 steps an
+    // instruction per step takes the 16 waves 0.24 us)
+    auto batch = [&](auto whole, int t0) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        uint32_t score[U], top = 0;
         int pos[U];
+        const float *scores = rows.scores + base + t0 * 64;
+        const int32_t *given = rows.pos + base + t0 * 64;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t0 + u < steps) {
-                const int j = min(base + (t0 + u) * 64, len - 1);
-                score[u] = rows.scores[j];
-                pos[u] = rows.pos_of(j);
-            }
+            if (WHOLE || t0 + u < steps) score[u] = __float_as_uint(WHOLE ? scores[u * 64] : rows.scores[min(base + (t0 + u) * 64, len - 1)]);
+        if (rows.pos) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (WHOLE || t0 + u < steps) pos[u] = WHOLE ? given[u * 64] : rows.pos[min(base + (t0 + u) * 64, len - 1)];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t0 + u < steps) {
-                uint32_t k = rows.key_of(score[u], pos[u]);
-                if (base + (t0 + u) * 64 >= len) k = kSafe;  // (counts as a protected one; `rank_of` is asked of tokens alone)
-                key[(t0 + u) * 64] = k;
+            if (WHOLE || t0 + u < steps) top = max(top, score[u]);
+        // no protected token, no negative score, -0 or NaN
+        const int j0 = first + t0 * 64, j1 = j0 + U * 64;
+        if (WHOLE && !rows.pos && j0 >= rows.sink && j1 <= rows.safe_from && __builtin_amdgcn_ballot_w64(top > 0x7f800000u) == 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t k = score[u] | 0x80000000u;
                 low = min(low, k);
-                above = max(above, k + 1);  // (0 of protected ones)
-                free_keys += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k != kSafe));
+                key[(t0 + u) * 64] = k;
             }
+            above = max(above, (top | 0x80000000u) + 1);
+            free_keys += U * 64;
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (WHOLE || t0 + u < steps) {
+                const int j = base + (t0 + u) * 64;
+                uint32_t k = rows.key_of(__uint_as_float(score[u]), rows.pos ? pos[u] : j);
+                if (!WHOLE && j >= len) k = kSafe;  // (counts as a protected one; `rank_of` is asked of tokens alone)
+                key[(t0 + u) * 64] = k;
+                count(k);
+            }
+    };
+    for (int t0 = 0; t0 < steps; t0 += U) {
+        if (t0 + U <= steps && first + (t0 + U) * 64 <= len) batch(std::true_type{}, t0);
+        else batch(std::false_type{}, t0);
     }
     if (holes()) {  // (behind a barrier)
         e.keep = len;
@@ -216,15 +249,29 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     }
     const int keep = e.keep, go = len - keep;
     auto rank_of = [&](int t, uint32_t k) { return Rank{rank_what(k, rows.pos_of(base + t * 64)), ~(uint32_t)(base + t * 64)}; };
-    low = reduce_lanes<1, 64>(low, OpMinU{});
-    above = reduce_lanes<1, 64>(above, OpMaxU{});
-    if (lane == 0) atomicMin(&sm.all_low, low), atomicMax(&sm.all_above, above), atomicAdd(&sm.all_free, free_keys);
+    auto of_all = [&] {
+        low = reduce_lanes<1, 64>(low, OpMinU{});
+        above = reduce_lanes<1, 64>(above, OpMaxU{});
+        if (lane == 0) atomicMin(&sm.all_low, low), atomicMax(&sm.all_above, above), atomicAdd(&sm.all_free, free_keys);
+        __syncthreads();
+        low = sm.all_low;
+        above = sm.all_above;
+        free_keys = sm.all_free;
+    };
     if (go > 1)
         for (int i = tid; i < kEvictBins; i += THREADS) sm.hist[i] = 0;
-    __syncthreads();
-    low = sm.all_low;
-    above = sm.all_above;
-    free_keys = sm.all_free;
+    of_all();
+    if (go > free_keys) {  // all that may go do, and protected ones by their position: other keys of the same order, positions in turns
+        __syncthreads();
+        if (tid == 0) sm.all_low = kSafe, sm.all_above = 0, sm.all_free = 0;
+        for (int t = 0; t < steps; ++t)
+            if (base + t * 64 < len)
+                key[t * 64] = key[t * 64] == kSafe ? min(max((uint32_t)rank_what(0, rows.pos_of(base + t * 64)), 1u), kSafe - 1) : 0u;
+        low = kSafe, above = 0, free_keys = 0;
+        for (int t = 0; t < steps; ++t) count(key[t * 64]);
+        __syncthreads();
+        of_all();
+    }
     Rank last;
     if (go == 1) {  // the smallest
         Rank best{~(uint64_t)0, ~0u};
@@ -253,11 +300,15 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
         if (tid == 0) e.move(0, gone, keep);
         return 1;
     }
+    // free places below `keep` and tokens that stay behind it are listed, both in order: steps with places below `keep`, the first step with others
+    const int front_steps = min(steps, max(0, keep - first + 63) / 64), back = min(steps, max(0, keep - first) / 64);
+    int gaps = 0, movers = 0;
     bool found = false;
-    if (go <= free_keys) {
+    {
         // one histogram, linear over that range; the bin of the last one to go; its keys ranked against each other
         const uint32_t range = above - 1 - low;
-        const uint32_t slope = range < kEvictBins ? 0u : (uint32_t)(((uint64_t)kEvictBins << 32) / ((uint64_t)range + 1));
+        // (a little less than kEvictBins 2^32 / (range + 1), which 64-bit division would take all waves 1.5 us for)
+        const uint32_t slope = range < kEvictBins ? 0u : (uint32_t)(kEvictBins * 0x1p32f * (1.f - 0x1p-20f) * __builtin_amdgcn_rcpf((float)range + 1.f));
         auto bin_of = [&](uint32_t k) { return (int)(slope ? __umulhi(k - low, slope) : k - low); };
 #pragma unroll 4
         for (int t = 0; t < steps; ++t) {
@@ -280,22 +331,48 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
                 if (go > below && go <= below + c[i]) sm.digit = tid * BPT + i, sm.rank = go - 1 - below, sm.in_bin = c[i];
                 below += c[i];
             }
+            // the bin's keys are those from `from` up to `to`; smaller ones go, larger ones stay
+            auto first_of = [&](int at) { return low + (slope ? (((uint64_t)at << 32) + slope - 1) / slope : (uint64_t)at); };
+            sm.from = (uint32_t)first_of(sm.digit);
+            sm.to = (uint32_t)min(first_of(sm.digit + 1) - 1, (uint64_t)(kSafe - 1));
         }
         __syncthreads();
-        const int bin = sm.digit, in_bin = sm.in_bin, want = sm.rank;
+        const int in_bin = sm.in_bin, want = sm.rank;
+        const uint32_t from = sm.from, to = sm.to;
         if (in_bin <= kEvictCandidates) {
             found = true;
-#pragma unroll 4
-            for (int t = 0; t < steps; ++t) {
+            auto note = [&](int t) {
                 const uint32_t k = key[t * 64];
-                if (k != kSafe && bin_of(k) == bin) sm.candidates[atomicAdd(&sm.n_candidates, 1)] = rank_of(t, k);
+                if (k >= from && k <= to) sm.candidates[atomicAdd(&sm.n_candidates, 1)] = rank_of(t, k);
+                return k;
+            };
+            int t = 0;
+#pragma unroll 8
+            for (; t < back; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(note(t) < from));
+            if (t < front_steps) {  // (the step that `keep` lies in)
+                const uint32_t k = note(t);
+                const int j = base + t * 64;
+                gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k < from && j < keep));
+                movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > to && j >= keep && j < len));
+                ++t;
             }
+#pragma unroll 8
+            for (; t < steps; ++t) {
+                uint64_t stays = __builtin_amdgcn_ballot_w64(note(t) > to);
+                if (first + t * 64 + 64 > len) stays &= ((uint64_t)1 << (len - first - t * 64)) - 1;
+                movers += __builtin_popcountll(stays);
+            }
+            if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
             __syncthreads();
             for (int i = tid; i < in_bin; i += THREADS) {
                 const Rank r = sm.candidates[i];
                 int smaller = 0;
                 for (int o = 0; o < in_bin; ++o) smaller += sm.candidates[o] < r;
                 if (smaller == want) sm.last = r;
+                // (what the rank says, too: the first want + 1 of them go)
+                const int j = (int)~r.place, w = j / per_wave;
+                if (smaller <= want && j < keep) atomicAdd(&sm.gaps[w], 1);
+                if (smaller > want && j >= keep) atomicAdd(&sm.movers[w], 1);
             }
             __syncthreads();
             last = sm.last;
@@ -309,24 +386,16 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
             const Rank r = sm.candidates[i];
             if ((uint32_t)(r.what >> 32) == last_key && last < r) keys[~r.place] = kSafe;
         }
-        __syncthreads();
     } else {
         last = last_to_go_by_digits(rows, len, go, sm);
         last_key = 0;
         for (int t = 0; t < steps; ++t)
-            if (base + t * 64 < len) key[t * 64] = last < rank_of(t, key[t * 64]) ? kSafe : 0u;
+            if (base + t * 64 < len) key[t * 64] = last < Rank{rank_what(rows.key_at(base + t * 64), rows.pos_of(base + t * 64)), ~(uint32_t)(base + t * 64)} ? kSafe : 0u;
+        for (int t = 0; t < front_steps; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[t * 64] == 0 && base + t * 64 < keep));
+        for (int t = back; t < steps; ++t)
+            movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[t * 64] != 0 && (uint32_t)(base + t * 64 - keep) < (uint32_t)go));
+        if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
     }
-    // free places below `keep` and tokens that stay behind it, both in order
-    const int front_steps = min(steps, max(0, keep - first + 63) / 64), back = min(steps, max(0, keep - first) / 64);  // steps with places below
-                                                                                                                        // `keep`, the first one with others
-    auto is_gap = [&](int t) { return key[t * 64] <= last_key && base + t * 64 < keep; };
-    auto is_mover = [&](int t) { return key[t * 64] > last_key && (uint32_t)(base + t * 64 - keep) < (uint32_t)go; };
-    int gaps = 0, movers = 0;
-#pragma unroll 8
-    for (int t = 0; t < front_steps; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is_gap(t)));
-#pragma unroll 8
-    for (int t = back; t < steps; ++t) movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is_mover(t)));
-    if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
     __syncthreads();
     gaps = movers = 0;
     int moved = 0;
@@ -339,14 +408,14 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     uint16_t *mover_places = gap_places + moved;
 #pragma unroll 8
     for (int t = 0; t < front_steps; ++t) {
-        const bool gap = is_gap(t);
+        const bool gap = key[t * 64] <= last_key && base + t * 64 < keep;
         const uint64_t m = __builtin_amdgcn_ballot_w64(gap);
         if (gap) gap_places[mask_number(m, gaps)] = (uint16_t)(base + t * 64);
         gaps += __builtin_popcountll(m);
     }
 #pragma unroll 8
     for (int t = back; t < steps; ++t) {
-        const bool mover = is_mover(t);
+        const bool mover = key[t * 64] > last_key && (uint32_t)(base + t * 64 - keep) < (uint32_t)go;
         const uint64_t m = __builtin_amdgcn_ballot_w64(mover);
         if (mover) mover_places[mask_number(m, movers)] = (uint16_t)(base + t * 64);
         movers += __builtin_popcountll(m);
