@@ -50,8 +50,10 @@ class Prompts:
     """Packed prompts on the host: `gap` rows before the first and behind the last one that belong to none, NaN in everything that
     no row may look at."""
 
-    def __init__(self, seed, lens, *, q_heads, kv_heads, d, dtype=torch.bfloat16, layout="thd", gap=0, scale=None, hot=0.0, pad=0):
+    def __init__(self, seed, lens, *, q_heads, kv_heads, d, dtype=torch.bfloat16, layout="thd", gap=0, scale=None, hot=0.0, pad=0,
+                 heads=None):
         self.lens, self.hq, self.hkv, self.d, self.dtype = lens, q_heads, kv_heads, d, dtype
+        self.heads = list(range(q_heads)) if heads is None else heads  # that are compared
         self.scale = d ** -0.5 if scale is None else scale
         self.tokens = sum(lens) + 2 * gap
         self.first = [gap + sum(lens[:s]) for s in range(len(lens) + 1)]
@@ -67,17 +69,18 @@ class Prompts:
             t[self.first[-1]:] = NAN
 
     def reference(self):
-        out, lse = np.full((self.tokens, self.hq, self.d), np.nan), np.full((self.hq, self.tokens), np.nan)
+        """Of the heads that are compared."""
+        out, lse = np.full((self.tokens, len(self.heads), self.d), np.nan), np.full((len(self.heads), self.tokens), np.nan)
         tol, ltol = np.zeros_like(out), np.zeros_like(lse)
         for lo, hi in zip(self.first, self.first[1:]):
             if hi == lo:
                 continue
             later = torch.ones(hi - lo, hi - lo, dtype=torch.bool).triu(1)
-            for h in range(self.hq):
+            for i, h in enumerate(self.heads):
                 kv = h * self.hkv // self.hq
                 o, t, l, lt = rows_of_attention(self.q[lo:hi, h].double(), self.k[lo:hi, kv].double(), self.v[lo:hi, kv].double(),
                                                 later, self.scale, self.dtype)
-                out[lo:hi, h], tol[lo:hi, h], lse[h, lo:hi], ltol[h, lo:hi] = o.numpy(), t.numpy(), l.numpy(), lt.numpy()
+                out[lo:hi, i], tol[lo:hi, i], lse[i, lo:hi], ltol[i, lo:hi] = o.numpy(), t.numpy(), l.numpy(), lt.numpy()
         return out, tol, lse, ltol
 
     def upload(self):
@@ -104,11 +107,13 @@ class Prompts:
         torch.cuda.synchronize()
         out, tol, lse, ltol = self.reference()
         got_out, got_lse = d["out"].float().cpu().numpy(), d["lse"].cpu().numpy()
-        none = np.isnan(lse[0])
+        none = np.ones(self.tokens, bool)
+        none[self.first[0]:self.first[-1]] = False
         assert np.isnan(got_out[none]).all() and np.isnan(got_lse[:, none]).all(), "rows that belong to no prompt are written"
-        some = torch.from_numpy(~none).cuda()
-        assert_within(d["out"][some], out[~none], tol[~none], "out")
-        assert_within(d["lse"][:, some], lse[:, ~none], ltol[:, ~none], "lse")
+        assert not np.isnan(got_out[~none]).any() and not np.isnan(got_lse[:, ~none]).any(), "rows are not written, or not numbers"
+        some, heads = torch.from_numpy(~none).cuda(), torch.tensor(self.heads).cuda()
+        assert_within(d["out"][some][:, heads], out[~none], tol[~none], "out")
+        assert_within(d["lse"][heads][:, some], lse[:, ~none], ltol[:, ~none], "lse")
         return d
 
 
