@@ -576,7 +576,7 @@ int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, 
  * Token j of sequence b has, for KV head h, its key and value in the pages, its running score in
  * scores[b, h, j] and its position in pos[b, h, j].  A sequence has tail_len[b] tokens (as
  * aha_append_paged counts them, the newest one last), clamped to what table and `slots` hold.  No page
- * may be in the tables of two sequences whose tokens are evicted.
+ * may occur twice among those of sequences whose tokens are evicted.
  */
 typedef struct aha_paged {
     int32_t batch;        /* batch * n_kv_heads <= 65535, batch * n_q_heads <= 2^22 */
@@ -641,7 +641,7 @@ int32_t aha_paged_attention(const aha_paged *p, const aha_pages *pages, const vo
  *  k_pages, v_pages  in place.
  *  scores_out, pos_out  out: what belongs to the tokens now in places below len_out[b]; places behind stay as
  *                they are.  Either may be its input (same pointer and strides); otherwise they must not overlap.
- *  len_out       out, DEVICE int32 [batch]; not tail_len.
+ *  len_out       out, DEVICE int32 [batch]; neither tail_len nor seen.
  * A sequence with a hole among its pages keeps all its tokens.
  */
 int32_t aha_paged_evict_workspace_bytes(const aha_paged *p, const aha_pages *pages, size_t *out_bytes);

@@ -494,7 +494,7 @@ int32_t aha_paged_evict(const aha_paged *p, const aha_pages *pages, const float 
         (rc = check_slots("scores", p->scores_stride, p, false)) || (pos && (rc = check_slots("pos", p->pos_stride, p, false))) ||
         (rc = check_slots("scores_out", p->scores_out_stride, p, true)) || (rc = check_slots("pos_out", p->pos_out_stride, p, true)))
         return rc;
-    if (len_out == tail_len) return fail(AHA_ERR_INVALID_ARG, "len_out is tail_len, which other workgroups still read");
+    if (len_out == tail_len || len_out == seen) return fail(AHA_ERR_INVALID_ARG, "len_out is tail_len or seen, which other workgroups still read");
     auto other_rows = [&](const int64_t a[2], const int64_t b[2]) {
         return (p->batch > 1 && a[0] != b[0]) || (p->n_kv_heads > 1 && a[1] != b[1]);
     };

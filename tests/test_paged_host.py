@@ -139,6 +139,7 @@ def test_pointers_and_workspaces():
     for name in ("scores", "k_pages", "v_pages", "page_table", "tail_len", "scores_out", "pos_out", "len_out"):
         assert evict(paged(), pages(), **{name: None}) == INVALID
     assert evict(paged(), pages(), len_out=PTR) == INVALID  # tail_len
+    assert evict(paged(), pages(), len_out=PTR, tail_len=OTHER) == INVALID  # seen
     n = ctypes.c_size_t(0)
     for call, size in ((attention, B.load().aha_paged_attention_workspace_bytes), (evict, B.load().aha_paged_evict_workspace_bytes)):
         assert size(ref(paged()), ref(pages()), ctypes.byref(n)) == B.AHA_OK and n.value % 256 == 0 and n.value > 0
