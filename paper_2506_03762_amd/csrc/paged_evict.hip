@@ -6,6 +6,7 @@
 // it moves the keys and values too where there can only be a few, else a second launch does.
 #include <limits.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "aha_dev.h"
@@ -506,11 +507,13 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictGeom g, E
     }
 }
 
-constexpr int kMoveRows = 16;  // of a workgroup
+// (more moves than the launch has rows for: workgroups take several lots)
+constexpr int kMoveRows = 16, kMoveWorkgroups = 1 << 16;  // of a lot; of a launch, at most, if every (sequence, KV head) gets one
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictGeom g, EvictPlan pl, const int32_t *counts, const int2 *moves) {
-    const int z = blockIdx.y, b = z / g.Hkv, first = blockIdx.x * kMoveRows;
-    const int count = min(kMoveRows, counts[z] - first);
-    move_rows(g, g.pages.table + (int64_t)b * g.pages.table_width, z % g.Hkv, moves + (int64_t)z * pl.moves + first, count, threadIdx.x, 256);
+    const int z = blockIdx.y, b = z / g.Hkv, count = counts[z];
+    for (int first = blockIdx.x * kMoveRows; first < count; first += gridDim.x * kMoveRows)
+        move_rows(g, g.pages.table + (int64_t)b * g.pages.table_width, z % g.Hkv, moves + (int64_t)z * pl.moves + first, min(kMoveRows, count - first),
+                  threadIdx.x, 256);
 }
 
 hipError_t launch_paged_evict(const EvictGeom &g, const EvictPlan &pl, void *ws, hipStream_t st) {
@@ -528,7 +531,8 @@ hipError_t launch_paged_evict(const EvictGeom &g, const EvictPlan &pl, void *ws,
     else select(evict_select_kernel<16>, 16);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.moves == 0 || pl.in_one) return e;
-    hipLaunchKernelGGL(evict_move_kernel, dim3((pl.moves + kMoveRows - 1) / kMoveRows, Z), dim3(256), 0, st, g, pl, counts, moves);
+    const int lots = std::min((pl.moves + kMoveRows - 1) / kMoveRows, std::max(1, kMoveWorkgroups / Z));
+    hipLaunchKernelGGL(evict_move_kernel, dim3(lots, Z), dim3(256), 0, st, g, pl, counts, moves);
     return hipGetLastError();
 }
 

@@ -96,6 +96,24 @@ def test_long_prompts(n):
     Evictions(17, [n], kv_heads=2, d=64, budget=n - 700, recent=64, scores=scores, pos=pos_of(1, 2, n), page=16, slots=n).check()
 
 
+def test_few_long_sequences_among_many():
+    """More (sequence, KV head) pairs than the moving launch has workgroups for all their moves."""
+    from paper_2506_03762_amd import binding as B
+    small = Evictions(20, [640, 600, 300], kv_heads=2, d=64, budget=280)
+    want, d = small.check(), small.upload()
+    batch, at = 4200, [0, 2500, 4199]
+    def wide(t, rest):
+        return torch.full((batch, *t.shape[1:]), rest, dtype=t.dtype, device="cuda").index_copy_(0, torch.tensor(at, device="cuda"), t)
+    table, scores, pos, tail = wide(d["table"], -1), wide(d["scores"], 1.0), wide(d["pos"], 5), wide(d["tail"], 0)
+    lens, cache = torch.full_like(tail, -7), B.Pages.of(d["k"], d["v"], table)
+    p = B.PagedEviction.of(scores, pos, scores, pos, cache, budget=280)
+    B.aha_paged_evict(p, cache, scores, pos, d["k"], d["v"], table, tail, None, scores, pos, lens, B.alloc_evict_workspace(p, cache))
+    assert torch.equal(lens, wide(want["len_out"], 0))
+    assert torch.equal(scores, wide(want["scores_out"], 1.0)) and torch.equal(pos, wide(want["pos_out"], 5))
+    for name in ("k", "v"):
+        assert torch.equal(d[name].view(torch.uint8), want[name].view(torch.uint8)), name
+
+
 def test_shared_scores():
     """One row of scores for all heads, expanded, into outputs of their own."""
     base = torch.rand(2, 1, 160, generator=torch.Generator().manual_seed(1))
