@@ -8,6 +8,12 @@ namespace aha {
 // Where the key and value rows of a range of keys lie: `entry` is what there is to know of a key beforehand (its page), `at` the rows'
 // offsets in elements from `k` and `v`; what is not there (beyond the end, in a hole) reads as zeros.
 __device__ __attribute__((aligned(256))) const uint32_t kZeroRow[128] = {};
+// A load from one of these: which of them a pointer is, the compiler cannot know, and its generic loads, which may be of LDS, are also counted with (and
+// waited for like) LDS reads (fp32: 7 caches of up to 901 tokens 13.3 us, so 12.9).
+template <class V>
+__device__ __forceinline__ V load_global(const void *p) {
+    return *(const __attribute__((address_space(1))) V *)(uintptr_t)p;
+}
 template <class T>
 struct KeyPlaces {
     const T *k, *v;

@@ -30,9 +30,9 @@ __device__ __forceinline__ void no_rows_yet(f32x16 (&O)[CB], float &m, float &s)
 #pragma unroll
         for (int v = 0; v < 16; ++v) O[cb][v] = 0.f;
 }
-// ONCE: the values are read past the caches, as no other tile reads them (64 caches of up to 4096 tokens, 8 heads of 128 160 us, so 156; the keys too
-// 191: a lane's pieces of a row come with eight loads, which then read it again).  `limit`: the last key that the lane's row sees.  `block(kb, acc)` is told the products of the 32 keys from kb on, those that a row does
-// not see -inf.
+// ONCE: the values are read past the caches, as no other tile reads them (64 caches of up to 4096 tokens, 8 x 4 heads of 128 channels 160 us, so 156; the
+// keys too 191: a lane's pieces of a row come with eight loads, which then read it again).  `limit`: the last key that the lane's row sees.
+// `block(kb, acc)` is told the products of the 32 keys from kb on, those that a row does not see -inf.
 template <int D, bool ONCE = false, class Keys, class Block>
 __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf)[D / 16], int limit, float c_out, char *smem, int lane, int wave,
                                              f32x16 (&O)[D / 32], float &m, float &s, Block block) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf
     bf16x8 a[KS];
     auto load_keys = [&](const __bf16 *k) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) a[ks] = *(const bf16x8 *)(k + hf * 8 + ks * 16);
+        for (int ks = 0; ks < KS; ++ks) a[ks] = load_global<bf16x8>(k + hf * 8 + ks * 16);
     };
 
     int kb = keys.begin + wave * 32;
@@ -152,9 +152,10 @@ __device__ __forceinline__ f32x16 dots_f32(const f32x4 (&a)[D / 8], const float 
     for (int v = 0; v < 16; ++v) acc[0][v] = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
     return acc[0];
 }
-// fp32: v_mfma_f32_32x32x2_f32; a lane's chunks of a key row and a query row as in f32_tile.h (`sq`: its row in LDS, from its half's first chunk on);
+// fp32: v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it beyond a few blocks' latency); a lane's chunks of a key row and a query row as in f32_tile.h (`sq`: its row in LDS, from its half's first chunk on);
 // the second product takes the weights from the accumulators one element at a time, a contraction step over the keys of the
-// two half-waves, and a value row's 32 channels per load straight from memory.
+// two half-waves, and a value row's 32 channels per load straight from memory.  With nothing requested ahead a prompt of 512 tokens, 2 heads of 64, took
+// 21.8 us, so 15.3.
 template <int D, class Keys, class Block>
 __device__ __forceinline__ void f32_sweep(const Keys &keys, const float *sq, int limit, float c_out, int lane, int wave, f32x16 (&O)[D / 32],
                                           float &m, float &s, Block block) {
@@ -169,7 +170,7 @@ __device__ __forceinline__ void f32_sweep(const Keys &keys, const float *sq, int
     f32x4 a[D / 8];
     auto load_keys = [&] {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) a[i] = *(const f32x4 *)(here.k + 4 * hf + 8 * i);
+        for (int i = 0; i < D / 8; ++i) a[i] = load_global<f32x4>(here.k + 4 * hf + 8 * i);
     };
     load_keys();
     for (; kb < keys.end; kb += A::STEP) {
@@ -181,7 +182,7 @@ __device__ __forceinline__ void f32_sweep(const Keys &keys, const float *sq, int
             const uint32_t lo = __shfl((uint32_t)mine, from), hi = __shfl((uint32_t)(mine >> 32), from);
             const float *vr = (const float *)(((uint64_t)hi << 32) | lo) + col;
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) v_row[v][cb] = vr[cb * 32];
+            for (int cb = 0; cb < CB; ++cb) v_row[v][cb] = load_global<float>(vr + cb * 32);
         };
         constexpr int AHEAD = D == 64 ? 16 : 0;  // (d = 128: they do not fit beside the dots' chains)
 #pragma unroll
@@ -281,6 +282,30 @@ __device__ __forceinline__ void meet_waves(int rows, bool live_row, f32x16 (&O)[
             for (int w = 0; w < A::WAVES; ++w) o += *(const f32x4 *)((const float *)smem + (w * 32 + q) * A::LDO + ch);
             store(q, hc * A::HC + ch, o);
         }
+    }
+}
+
+// LDS of a kernel of these sweeps: the values' blocks (fp32: the query rows), later the waves' results.
+template <class T, int D>
+constexpr size_t narrow_lds() {
+    const size_t swept = sizeof(T) == 2 ? NarrowRows<D>::stage_bytes : (size_t)32 * f32_ld(D) * 4;
+    return swept > WaveMerge<D>::bytes ? swept : WaveMerge<D>::bytes;
+}
+// Its workgroups per CU, at least.  Three where their LDS (32 KB each) and registers allow it without spills, bf16 with d = 64: there latency is what a
+// block of keys mostly waits for (16 prompts of 200 tokens, 6 heads over 2: 9.3 us, with two 11.2; 64 caches of up to 4096 tokens, 8 x 4 heads 60.5 and 62.9;
+// with four the registers spill).
+template <class T, int D>
+constexpr int kNarrowWorkgroups = sizeof(T) == 2 && D == 64 ? 3 : 2;
+// Query row `q` of lane % 32 (its 16-byte fragments, or zeros) to the tile's rows in LDS, fp32: wave w takes channels [w D / 4, + D / 4) of all rows, the
+// half-waves alternate.
+template <int D>
+__device__ __forceinline__ void stage_f32_rows(float *sq, const float *q, bool live, int lane, int wave) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const int c = wave * (D / 4) + i * 8 + (lane >> 5) * 4;
+        f32x4 x = *(const f32x4 *)(q + c);
+        if (!live) x = f32x4{};
+        *(f32x4 *)(sq + (lane & 31) * f32_ld(D) + c) = x;
     }
 }
 

@@ -27,20 +27,10 @@ __device__ __forceinline__ int64_t paged_partial(const PagedGeom &g, const Paged
 }
 
 template <class T, int D>
-struct PagedLds;
-template <int D>
-struct PagedLds<__bf16, D> {
-    static constexpr size_t bytes = NarrowRows<D>::stage_bytes > WaveMerge<D>::bytes ? NarrowRows<D>::stage_bytes : WaveMerge<D>::bytes;
-};
-template <int D>
-struct PagedLds<float, D> {
-    static constexpr size_t q_bytes = (size_t)32 * f32_ld(D) * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
-};
-
-template <class T, int D>
-__global__ __launch_bounds__(256, 2) void paged_part_kernel(PagedGeom g, PagedPlan pl, float *part_o, float2 *part_ms, float2 *part_ms2, float *dots) {
+__global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_kernel(PagedGeom g, PagedPlan pl, float *part_o, float2 *part_ms,
+                                                                              float2 *part_ms2, float *dots) {
     constexpr int STEP = NarrowRows<D>::STEP;
-    __shared__ __attribute__((aligned(1024))) char smem[PagedLds<T, D>::bytes];
+    __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<T, D>()];
     __shared__ float2 s_ms2[4][32];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     // (sequence, KV head) by part by tile
@@ -93,13 +83,7 @@ __global__ __launch_bounds__(256, 2) void paged_part_kernel(PagedGeom g, PagedPl
         narrow_sweep<D, true>(keys, qf, INT_MAX, g.c_out, smem, lane, wave, O, m, s, block);
     } else {
         float *sQ = (float *)smem;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
-            const int c = wave * (D / 4) + i * 8 + hf * 4;
-            f32x4 x = *(const f32x4 *)(q + c);
-            if (!live) x = f32x4{};
-            *(f32x4 *)(sQ + col * f32_ld(D) + c) = x;
-        }
+        stage_f32_rows<D>(sQ, q, live, lane, wave);
         __syncthreads();
         f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, INT_MAX, g.c_out, lane, wave, O, m, s, block);
     }

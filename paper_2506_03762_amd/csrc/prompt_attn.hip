@@ -11,21 +11,10 @@
 
 namespace aha {
 
-template <class T, int D>
-struct PromptLds;
-template <int D>
-struct PromptLds<__bf16, D> {
-    static constexpr size_t bytes = NarrowRows<D>::stage_bytes > WaveMerge<D>::bytes ? NarrowRows<D>::stage_bytes : WaveMerge<D>::bytes;
-};
-template <int D>
-struct PromptLds<float, D> {
-    static constexpr size_t q_bytes = (size_t)32 * f32_ld(D) * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
-};
-
 // ---- tiles of 32 rows ----
 template <class T, int D>
-__global__ __launch_bounds__(256, 2) void prompt_narrow_kernel(PromptGeom g) {
-    __shared__ __attribute__((aligned(1024))) char smem[PromptLds<T, D>::bytes];
+__global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_kernel(PromptGeom g) {
+    __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<T, D>()];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     PromptTile it;
     if (!prompt_tile(g, 32, (int)blockIdx.x, lane, it)) return;
@@ -46,11 +35,7 @@ __global__ __launch_bounds__(256, 2) void prompt_narrow_kernel(PromptGeom g) {
         narrow_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s, [](int, const f32x16 &) {});
     } else {
         float *sQ = (float *)smem;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
-            const int c = wave * (D / 4) + i * 8 + hf * 4;
-            *(f32x4 *)(sQ + col * f32_ld(D) + c) = *(const f32x4 *)(q + c);
-        }
+        stage_f32_rows<D>(sQ, q, true, lane, wave);
         __syncthreads();
         f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, limit, g.c_out, lane, wave, O, m, s, [](int, const f32x16 &) {});
     }

@@ -27,21 +27,17 @@ __device__ __forceinline__ void merge_waves(const SharedGeom &g, const SharedPla
 // Four waves take blocks of 32 keys in turn, each with all rows: a stream of keys and values, bound by memory.  Per block and
 // wave: S^T = K Q^T and O^T += V^T P^T by v_mfma_f32_32x32x16_bf16, keys (channels) on M, rows on N, so that the accumulator elements of a
 // lane are the probabilities that it supplies to the second product.  Keys go to registers, values to LDS, both a block ahead: 64 KB
-// of requests per workgroup (d = 128), two of them per CU.  64 sequences of four prefixes of 4096 tokens, tails of up to 1001: 203 MB from memory (each prefix once:
-// the second tile of its 64 rows finds it in the L2) in 52 us, 3.9 TB/s; what is missing of 4.8 are the items' starts, 4 to 6 us each, and the last
+// of requests per workgroup (d = 128), two of them per CU.  64 sequences of four prefixes of 4096 tokens, tails of up to 1001: 203 MB from memory (each prefix
+// once: the second tile of its 64 rows finds it in the L2) in 52 us, 3.9 TB/s; what is missing of 4.8 are the items' starts, 4 to 6 us each, and the last
 // tails.  8 sequences of one prefix of 2048: 9.4 us, a chain of five round trips.
 // The weights are rounded to bf16 for the second product, as the matrix core takes them beside bf16 values (their sum is of the unrounded ones, in fp32):
 // outputs are 0.0018 to 0.0023 from 64 bits, relative to their size, where a single rounding of the exact ones is 0.0017.  Weights in two
 // parts would double that product.
 template <int D>
-struct NarrowAttn : NarrowRows<D> {
-    static constexpr size_t bytes = NarrowRows<D>::stage_bytes > WaveMerge<D>::bytes ? NarrowRows<D>::stage_bytes : WaveMerge<D>::bytes;
-};
-template <int D>
 __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
-    using A = NarrowAttn<D>;
+    using A = NarrowRows<D>;
     constexpr int KS = D / 16, CB = D / 32;
-    __shared__ __attribute__((aligned(1024))) char smem[A::bytes];
+    __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<__bf16, D>()];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     SharedItem it;
     if (!shared_item(g, pl, (int)blockIdx.x, 32, A::STEP, lane, it)) return;
@@ -70,21 +66,12 @@ __global__ __launch_bounds__(256, 2) void shared_narrow_kernel(SharedGeom g, Sha
 }
 
 // ---- fp32 ----
-// The same on v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it): a lane's chunks of a key row and a query
-// row as in f32_tile.h; the second product takes the probabilities from the accumulators one element at a time, a
-// contraction step over the keys of the two half-waves, and a value row's 32 channels per load straight from memory.  Beyond a few workgroups' latency
-// the loads bound it: a block's page, keys and values are requested one after the other, none ahead (2 x 64 rows x 4 heads, 4096 keys, d = 128: products
-// 7 of 49 us).
-template <int D>
-struct F32Attn {
-    static constexpr int WAVES = 4, STEP = 32 * WAVES, LDQ = f32_ld(D);
-    static constexpr size_t q_bytes = (size_t)32 * LDQ * 4, bytes = q_bytes > WaveMerge<D>::bytes ? q_bytes : WaveMerge<D>::bytes;
-};
+// The same on v_mfma_f32_32x32x2_f32 (narrow_tile.h).
 template <int D>
 __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, SharedPlan pl, float *part_o, float2 *part_ms) {
-    using A = F32Attn<D>;
+    using A = NarrowRows<D>;
     constexpr int CB = D / 32;
-    __shared__ __attribute__((aligned(16))) char smem[A::bytes];
+    __shared__ __attribute__((aligned(16))) char smem[narrow_lds<float, D>()];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     SharedItem it;
     if (!shared_item(g, pl, (int)blockIdx.x, 32, A::STEP, lane, it)) return;
@@ -95,18 +82,9 @@ __global__ __launch_bounds__(256, 2) void shared_f32_kernel(SharedGeom g, Shared
     }
     const SharedKeys<float> keys(g, it);
     float *sQ = (float *)smem;
-    {  // wave w: channels [w D / 4, + D / 4) of all rows, the half-waves alternate
-        const float *p = (const float *)g.q + row.b * g.qs[0] + row.hq * g.qs[1] + row.t * g.qs[2];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            const int c = wave * (D / 4) + i * 8 + hf * 4;
-            f32x4 x = *(const f32x4 *)(p + c);
-            if (!row.live) x = f32x4{};
-            *(f32x4 *)(sQ + col * A::LDQ + c) = x;
-        }
-    }
+    stage_f32_rows<D>(sQ, (const float *)g.q + row.b * g.qs[0] + row.hq * g.qs[1] + row.t * g.qs[2], row.live, lane, wave);
     __syncthreads();
-    const float *sq = sQ + col * A::LDQ + 4 * hf;
+    const float *sq = sQ + col * f32_ld(D) + 4 * hf;
     const float c_out = pl.c_out;
     const int limit = row.limit;
     f32x16 O[CB];

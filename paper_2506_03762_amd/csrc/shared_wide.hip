@@ -1,6 +1,5 @@
-// Attention behind shared prefixes where many rows see the same keys: bf16, 65 rows and more (shared_attn.hip says what is computed).
-//
-// (wide_tile.h says how.)
+// Attention behind shared prefixes where many rows see the same keys: bf16, 65 rows and more (shared_attn.hip says what is computed,
+// wide_tile.h how).
 //
 // 4 x 256 rows of 32 heads, 16384 keys: 373 us with all loads of a stage issued together and the largest logit taken in every block; 352 with
 // the loads between the products; 311 with their addresses advanced in the vector ALU and a plain loop; now 304, 925 TFLOP/s with both launches

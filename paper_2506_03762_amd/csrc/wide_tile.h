@@ -61,10 +61,10 @@ struct WideRows {
     static_assert(bytes <= 160 * 1024 && KEYS % (RPI * WAVES) == 0, "one CU's LDS, whole instructions per wave");
 };
 
-
 // The sweep.  `in_a_row`: the keys lie token by token, else in pages: entry(key) is the page of a key before the end, `holes`: one of them may be
 // none.  `rows()` requests the wave's query rows and says the last key that each row sees and the least of these of either block;
-// `take(n)`, n loads later, has them in the fragments qf.  `mine()`: blocks of 32 keys that the wave's rows see (0: it has no rows).  O, m and s are the wave's, s per half-wave.
+// `take(n)`, n loads later, has them in the fragments qf.  `mine()`: blocks of 32 keys that the wave's rows see (0: it has no rows).  O, m and s are the
+// wave's, s per half-wave.
 template <int D, int RW, class Entry, class Rows, class Take, class Mine>
 __device__ __forceinline__ void wide_sweep(const KeyPlaces<__bf16> &keys, bool in_a_row, bool holes, Entry entry, char *smem, int lane, int wave,
                                            float c_out, bf16x8 (&qf)[2][D / 16], int (&limit)[2], int (&limit_min)[2], f32x16 (&O)[2][D / 32],
