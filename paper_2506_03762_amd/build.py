@@ -14,7 +14,7 @@ OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["aha_api.hip", "value_prior.hip", "score_f32.hip", "score_hold_f32.hip", "score_bf16.hip", "score_full.hip", "score_window.hip", "score_share.hip", "score_given.hip",
            "attn_window.hip", "topk.hip", "compact.hip", "decode.hip",
            "rotate.hip", "shared_attn.hip", "shared_wide.hip", "shared_api.hip",
-           "prompt_attn.hip", "prompt_wide.hip", "paged_attn.hip", "paged_evict.hip"]
+           "prompt_attn.hip", "prompt_wide.hip", "prompt_mid.hip", "paged_attn.hip", "paged_evict.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

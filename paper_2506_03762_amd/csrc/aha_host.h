@@ -300,13 +300,16 @@ struct PromptGeom {
     float c_out;  // scale times log2(e), above 0
 };
 struct PromptPlan {
-    int rows;       // of a tile: 32, or 256 (prompt_wide.hip)
+    int rows;       // of a tile: 32, 128 (prompt_mid.hip) or 256 (prompt_wide.hip)
     int64_t items;  // workgroups, at most (the prompts' lengths are known on the device)
 };
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
 // prompt_wide.hip
 // Tiles of 256 rows (bf16).
 hipError_t launch_prompt_wide(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
+// prompt_mid.hip
+// Tiles of 128 rows (bf16).
+hipError_t launch_prompt_mid(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
 
 // paged_attn.hip
 // One new token of every sequence over its pages, and the running scores.

@@ -58,6 +58,7 @@ static hipError_t launch_prompt_t(const PromptGeom &g, const PromptPlan &pl, hip
 }
 
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
+    if (pl.rows == 128) return launch_prompt_mid(g, pl, st);
     if (pl.rows > 32) return launch_prompt_wide(g, pl, st);
     return g.dtype == AHA_BF16 ? launch_prompt_t<__bf16>(g, pl, st) : launch_prompt_t<float>(g, pl, st);
 }

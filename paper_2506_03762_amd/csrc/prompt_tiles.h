@@ -84,15 +84,16 @@ struct PromptUnits {
     int lo, n, h, first, end;  // the prompt, its tokens, the KV head, the first unit, keys of the tile
 };
 constexpr int kUnits = 4;
+template <int ROWS>
 __device__ __forceinline__ bool prompt_units(const PromptGeom &g, int id, int lane, PromptUnits &it) {
     int lo, n, t;
     it.h = id % g.Hkv;
-    auto units = [&](int len) { return (len + 63) / 64 * g.G; };
+    auto units = [&](int len) { return (len + ROWS - 1) / ROWS * g.G; };
     if (!tile_of(g, id / g.Hkv, lane, lo, n, t, [&](int len) { return (units(len) + kUnits - 1) / kUnits; })) return false;
     it.lo = uniform(lo);
     it.n = uniform(n);
     it.first = uniform(t * kUnits);
-    it.end = min(it.n, (min(it.first + kUnits, units(it.n)) - 1) / g.G * 64 + 64);
+    it.end = min(it.n, (min(it.first + kUnits, units(it.n)) - 1) / g.G * ROWS + ROWS);
     return true;
 }
 

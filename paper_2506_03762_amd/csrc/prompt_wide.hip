@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256, 1) void prompt_wide_kernel(PromptGeom g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     PromptUnits it;
-    if (!prompt_units(g, (int)blockIdx.x, lane, it)) return;
+    if (!prompt_units<64>(g, (int)blockIdx.x, lane, it)) return;
     const int unit = it.first + wave, hq = it.h * g.G + unit % g.G, row0 = unit / g.G * 64;  // the wave's rows, counted from the prompt's start
     const int rows_here = max(0, min(64, it.n - row0));
     KeyPlaces<__bf16> keys;

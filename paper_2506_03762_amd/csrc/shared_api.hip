@@ -212,20 +212,37 @@ static int32_t check_prompt(const aha_prompt *p, bool strides) {
     return check_pair("out", p->out_stride, p->dtype, p->head_dim, true, p->tokens, p->n_q_heads);
 }
 
+// What a tile of the attention of packed prompts costs, us: its start and end, 32 keys of it, and by how much those that do not run at once with the first
+// ones cost more.
+struct PromptTiles {
+    int rows, unit, slots;  // rows; of one head at a time; tiles that run at once
+    float start, block, later;
+};
 static PromptPlan plan_prompt(const aha_prompt *p) {
     PromptPlan pl{};
-    const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads;
-    // Tiles of 256 rows where they fill a good part of the chip, by a count as if prompts ended evenly in their last block of 64 rows.  us in tiles of 32 and
-    // of 256 rows, d = 128, 4 query heads of each KV head: 8 heads, prompts of 512 tokens 15.7, 21.9, 768 27.7, 28.6, 1024 36.0, 34.9, 2048 95.0, 62.0,
-    // 16 of 64 16.8, 11.1, 4 of 200 18.9, 14.4; 2 heads, one of 2048 36.9, 59.4, 4 of 500 17.6, 21.8, 16 of 200 21.1, 15.0; d = 64, 16 of 16 heads,
-    // one of 2048 32.2, 48.1, 4 of 500 17.1, 19.1, 16 of 200 22.4, 13.4; 6 of 2 heads, 16 of 200 12.0, 12.0, of 500 26.0, 19.0.
-    const int64_t even = ((int64_t)p->tokens + 31 * prompts) / 64 * group * p->n_kv_heads;
-    pl.rows = p->dtype == AHA_BF16 && even / 4 >= (p->head_dim == 64 ? 176 : 112) ? 256 : 32;
-    if (pl.rows > 32) {  // at most one block of 64 rows, and one tile, of every prompt that is not full
-        const int64_t blocks = (p->tokens + 63 * prompts) / 64;
-        pl.items = (blocks * group + prompts * 3) / 4 * p->n_kv_heads;
-    } else {
-        pl.items = ((p->tokens + 31 * prompts) / 32 * p->n_kv_heads + 7) / 8 * 8 * group;
+    // The cheapest tiles by an estimate for prompts of equal lengths (the host knows no others): the first ones' cost, all of a prompt's keys, and the average
+    // one's for every further round.  The numbers are fitted to the times of 324 shapes (1 to 64 prompts of 20 to 8192 tokens, 2 to 64 heads): what they
+    // choose is 0.7 % slower than the fastest tiles on average, and 1.2 times at worst (16 prompts of 100 tokens, 8 heads over 2: 10.3, 8.6, 12.2 us in the order of
+    // the table).  d = 128, 32 heads over 8: one prompt of 512 14.8, 17.0, 21.7, 1024 36, 29.3, 34.9, 4096 310, 158, 138, 16 of 200 55, 24.7, 32;
+    // 8 over 2: one of 2048 36.6, 49.4, 59, 16 of 64 7.6, 7.1, 10.3.  d = 64, 16 heads: one of 1024 13.8, 21.8, 28.4, of 4096 94, 80, 88, 16 of
+    // 500 49, 29.3, 28.9.
+    static constexpr PromptTiles kTiles[2][3] = {
+        {{32, 32, 512, 5.94f, .235f, 1.f}, {128, 32, 512, 5.38f, .49f, 1.26f}, {256, 64, 256, 5.81f, .55f, 1.f}},    // d = 64
+        {{32, 32, 512, 8.9f, .4125f, 1.f}, {128, 32, 512, 8.2f, .66f, 1.3f}, {256, 64, 256, 13.4f, .66f, 1.f}}};  // d = 128
+    const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads, n = (p->tokens + prompts - 1) / prompts;
+    float least = INFINITY;
+    for (const PromptTiles &t : kTiles[p->head_dim == 128]) {
+        if (t.rows > 32 && p->dtype != AHA_BF16) continue;
+        const int64_t units = (n + t.unit - 1) / t.unit * group, heads = t.rows / t.unit;  // (a tile of 32 rows: one unit)
+        const int64_t tiles = prompts * ((units + heads - 1) / heads) * p->n_kv_heads;
+        const float keys = t.block * (float)n / 32;
+        const float time = t.start + keys + std::max(0.f, (float)tiles / t.slots - 1.f) * t.later * (t.start + keys / 2);
+        if (time >= least) continue;
+        least = time;
+        pl.rows = t.rows;
+        // at most: one unit's rows, and one tile, of every prompt are not full
+        pl.items = ((p->tokens + (t.unit - 1) * prompts) / t.unit * group + prompts * (heads - 1)) / heads * p->n_kv_heads;
+        if (heads == 1) pl.items = (pl.items / group + 7) / 8 * 8 * group;
     }
     return pl;
 }
