@@ -326,6 +326,7 @@ struct PagedGeom {
 };
 struct PagedPlan {
     int tiles, parts;   // of 32 rows of a (sequence, KV head), of its keys
+    bool one;           // launch: there is one part, and one tile
     int64_t items, ld;  // workgroups; floats of a row of dots
     size_t off_ms, off_ms2, off_dots, bytes;  // behind the partial outputs: references and sums, of the output's weights and of the scores'
 };

@@ -4,7 +4,12 @@
 //
 // in two launches.  The first takes the keys of a (sequence, KV head) in parts: the rows of its query heads, padded to a tile of 32, in one pass
 // over the part's keys and values (narrow_tile.h), which leaves the products, a partial output and the sums of both softmaxes, relative
-// to references of their own, in the workspace.  The second joins the parts: outputs by row, scores by range of keys.
+// to references of their own, in the workspace.  The second joins the parts: outputs by row, scores by range of keys.  Where there is one part, its
+// workgroup does that itself (plan_paged() says when).
+//
+// Bound by memory: keys and values are read once, for all query heads of their KV head, and two operations per element and head are far below what the
+// matrix core gives.  64 caches of up to 4096 tokens, 8 heads of 128: 670 MB in 145 us, 4.6 TB/s (a copy reaches 4.95), joining 12 more; one cache of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.6 + 4.5, of which 14 are the
+// 67 MB.  Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
 #include <limits.h>
 
 #include "narrow_tile.h"
@@ -26,12 +31,63 @@ __device__ __forceinline__ int64_t paged_partial(const PagedGeom &g, const Paged
     return ((int64_t)z * pl.parts + part) * g.G + gi;
 }
 
-template <class T, int D>
+// The scores of four tokens from j0 on: `dot` the products of the first U rows, `score` and `page` what the tokens have (places past the last one: anything),
+// `norm` reference and 1 / sum of every row.
+constexpr int kScoreRows = 4;  // rows whose products are in flight at once
+struct ScoreLoads {
+    f32x4 dot[kScoreRows];
+    float score[4];
+    int page[4];
+    // (nothing of the sequence's length: places lie within the workspace's rows, the table and the scores wherever its end is)
+    __device__ __forceinline__ void request(const PagedGeom &g, const float *x, int64_t ld, const float *F, const int32_t *table, int at) {
+#pragma unroll
+        for (int u = 0; u < kScoreRows; ++u) dot[u] = *(const f32x4 *)(x + min(u, g.G - 1) * ld + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            score[i] = F[min(at + i, g.slots - 1)];
+            page[i] = table[min((at + i) >> g.pages.page_shift, g.pages.table_width - 1)];
+        }
+    }
+    __device__ __forceinline__ void add(const PagedGeom &g, const float *x, int64_t ld, float *F, int32_t *pos, int at, int j0, int len, int seen, float lam,
+                                        const float2 *norm) {
+        float w[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int g0 = 0; g0 < g.G; g0 += kScoreRows) {
+            if (g0) {
+#pragma unroll
+                for (int u = 0; u < kScoreRows; ++u) dot[u] = *(const f32x4 *)(x + min(g0 + u, g.G - 1) * ld + at);
+            }
+#pragma unroll
+            for (int u = 0; u < kScoreRows; ++u)
+                if (g0 + u < g.G) {
+                    const float2 n = norm[g0 + u];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] += fast_exp2(fmaf(dot[u][i], lam, -n.x)) * n.y;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + i;
+            if (j >= len) break;
+            const bool there = page[i] >= 0 && page[i] < g.pages.n_pages;
+            if (j == len - 1) {
+                F[j] = there ? w[i] : 0.f;
+                if (pos) pos[j] = seen - 1;
+            } else if (there) {
+                F[j] = score[i] + w[i];
+            }
+        }
+    }
+};
+// Reference and 1 / sum of a row's weights (NaN stays).
+__device__ __forceinline__ float2 score_norm(float ref, float all) { return make_float2(ref, all > 0.f ? 1.f / all : all == 0.f ? 0.f : all); }
+
+// ONE: all keys are one part, whose outputs and scores are formed here.
+template <class T, int D, bool ONE>
 __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_kernel(PagedGeom g, PagedPlan pl, float *part_o, float2 *part_ms,
                                                                               float2 *part_ms2, float *dots) {
     constexpr int STEP = NarrowRows<D>::STEP;
     __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<T, D>()];
-    __shared__ float2 s_ms2[4][32];
+    __shared__ float2 s_ms2[4][32], s_norm[32];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     // (sequence, KV head) by part by tile
     const int id = blockIdx.x, tile = id % pl.tiles, part = id / pl.tiles % pl.parts, z = id / pl.tiles / pl.parts;
@@ -44,7 +100,11 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_ker
     keys.begin = (int)((int64_t)part * steps / pl.parts) * STEP;
     keys.end = min(len, (int)((int64_t)(part + 1) * steps / pl.parts) * STEP);
     if (keys.begin >= keys.end) {
-        if (tid < rows) {
+        if constexpr (ONE) {
+            for (int i = tid; i < rows * (D / 4); i += 256)
+                store_output((T *)g.out + b * g.os[0] + (h * g.G + i / (D / 4)) * g.os[1] + i % (D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f);
+            if (tid < rows && g.lse) g.lse[(int64_t)b * g.Hq + h * g.G + tid] = -INFINITY;
+        } else if (tid < rows) {
             part_ms[paged_partial(g, pl, z, part, row0 + tid)] = make_float2(-INFINITY, 0.f);
             if (dots) part_ms2[paged_partial(g, pl, z, part, row0 + tid)] = make_float2(-INFINITY, 0.f);
         }
@@ -92,11 +152,13 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_ker
         const float all = combine_lane_xor<32>(s2 * fast_exp2(m2 - ref), OpSum{});
         if (lane < 32) s_ms2[wave][lane] = make_float2(M, all);
     }
+    const float *sums = (const float *)(smem + WaveMerge<D>::off_sums);
     meet_waves<D>(
         rows, live, O, m, s, smem, lane, wave,
         [&](float M, float all) {
             const int64_t p = paged_partial(g, pl, z, part, gi);
-            part_ms[p] = make_float2(M, all);
+            if constexpr (!ONE) part_ms[p] = make_float2(M, all);
+            else if (g.lse) g.lse[(int64_t)b * g.Hq + hq] = all == 0.f ? -INFINITY : (M + log2f(all)) * kLn2;
             if (!dots) return;
             float M2 = -INFINITY, all2 = 0.f;
 #pragma unroll
@@ -104,9 +166,29 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_ker
             const float ref = M2 == -INFINITY ? 0.f : M2;
 #pragma unroll
             for (int w = 0; w < 4; ++w) all2 = fmaf(fast_exp2(s_ms2[w][col].x - ref), s_ms2[w][col].y, all2);
-            part_ms2[p] = make_float2(M2, all2);
+            if constexpr (ONE) s_norm[col] = score_norm(ref, all2);
+            else part_ms2[p] = make_float2(M2, all2);
         },
-        [&](int r, int ch, const f32x4 &o) { *(f32x4 *)(part_o + paged_partial(g, pl, z, part, row0 + r) * D + ch) = o; });
+        [&](int r, int ch, const f32x4 &o) {
+            if constexpr (ONE) {
+                const float all = sums[r];
+                store_output((T *)g.out + b * g.os[0] + (h * g.G + r) * g.os[1] + ch, o, all == 0.f ? 0.f : 1.f / all);
+            } else {
+                *(f32x4 *)(part_o + paged_partial(g, pl, z, part, row0 + r) * D + ch) = o;
+            }
+        });
+    if constexpr (ONE) {
+        if (!dots) return;
+        __syncthreads();  // the products of all waves, and s_norm
+        const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld;
+        const int seen = (g.seen ? g.seen : g.pages.tail_len)[b];
+        for (int j0 = 4 * tid; j0 < len; j0 += 1024) {
+            float *F = g.scores + b * g.ss[0] + h * g.ss[1];
+            ScoreLoads l;
+            l.request(g, x, pl.ld, F, keys.table, j0);
+            l.add(g, x, pl.ld, F, g.pos ? g.pos + b * g.ps[0] + h * g.ps[1] : nullptr, j0, j0, len, seen, lam, s_norm);
+        }
+    }
 }
 
 // ---- joining ----
@@ -151,66 +233,33 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedGeom g, PagedPlan 
         if (g.lse && ch == 0) g.lse[(int64_t)b * g.Hq + hq] = x.s == 0.f ? -INFINITY : (x.m + log2f(x.s)) * kLn2;
         return;
     }
-    // ---- scores: a thread takes four tokens ----
-    // (the products of the first rows, scores and pages are requested before anything of the sequence is known: they lie within the
-    // workspace's rows, the table and scores wherever its end is)
-    __shared__ float2 norm[kMaxGroup];  // of every row: reference, 1 / sum
+    // ---- scores: a thread takes four tokens (requested before anything of the sequence is known) ----
+    __shared__ float2 norm[kMaxGroup];
     const int lane = tid & 63, j0 = (blockIdx.x - out_wgs) * kJoinKeys + 4 * tid, at = min(j0, (int)pl.ld - 4);
-    const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld + at;
+    const float *x = dots + ((int64_t)b * g.Hq + (int64_t)h * g.G) * pl.ld;
     float *F = g.scores + b * g.ss[0] + h * g.ss[1];
-    const int32_t *table = g.pages.table + (int64_t)b * g.pages.table_width;
-    f32x4 dot[U];
-    float score[4];
-    int page[4];
-#pragma unroll
-    for (int u = 0; u < U; ++u) dot[u] = *(const f32x4 *)(x + min(u, g.G - 1) * pl.ld);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        score[i] = F[min(at + i, g.slots - 1)];
-        page[i] = table[min((at + i) >> g.pages.page_shift, g.pages.table_width - 1)];
-    }
+    ScoreLoads l;
+    l.request(g, x, pl.ld, F, g.pages.table + (int64_t)b * g.pages.table_width, at);
     const int len = tokens_of(g, b), seen = (g.seen ? g.seen : g.pages.tail_len)[b];
     if ((blockIdx.x - out_wgs) * kJoinKeys >= len) return;
     for (int gi = tid >> 6; gi < g.G; gi += 4) {  // (up to 64 parts, one per lane)
         const float2 ms = lane < pl.parts ? part_ms2[paged_partial(g, pl, z, lane, gi)] : make_float2(-INFINITY, 0.f);
         const float M = wave_max(ms.x), ref = M == -INFINITY ? 0.f : M, all = wave_sum(fast_exp2(ms.x - ref) * ms.y);
-        if (lane == 0) norm[gi] = make_float2(ref, all > 0.f ? 1.f / all : all == 0.f ? 0.f : all);  // (NaN stays)
+        if (lane == 0) norm[gi] = score_norm(ref, all);
     }
     __syncthreads();
-    const float lam = score_scale(g, b);
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int g0 = 0; g0 < g.G; g0 += U) {
-        if (g0) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) dot[u] = *(const f32x4 *)(x + min(g0 + u, g.G - 1) * pl.ld);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (g0 + u < g.G) {
-                const float2 n = norm[g0 + u];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] += fast_exp2(fmaf(dot[u][i], lam, -n.x)) * n.y;
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + i;
-        if (j >= len) break;
-        const bool there = page[i] >= 0 && page[i] < g.pages.n_pages;
-        if (j == len - 1) {
-            F[j] = there ? w[i] : 0.f;
-            if (g.pos) g.pos[b * g.ps[0] + h * g.ps[1] + j] = seen - 1;
-        } else if (there) {
-            F[j] = score[i] + w[i];
-        }
-    }
+    l.add(g, x, pl.ld, F, g.pos ? g.pos + b * g.ps[0] + h * g.ps[1] : nullptr, at, j0, len, seen, score_scale(g, b), norm);
 }
 
 template <class T, int D>
 static hipError_t launch_paged_t(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st) {
     float *part_o = (float *)ws, *dots = g.slots > 0 ? (float *)((char *)ws + pl.off_dots) : nullptr;
     float2 *part_ms = (float2 *)((char *)ws + pl.off_ms), *part_ms2 = (float2 *)((char *)ws + pl.off_ms2);
-    hipLaunchKernelGGL((paged_part_kernel<T, D>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
+    if (pl.one) {
+        hipLaunchKernelGGL((paged_part_kernel<T, D, true>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((paged_part_kernel<T, D, false>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int score_wgs = g.slots > 0 ? (int)((pl.ld + kJoinKeys - 1) / kJoinKeys) : 0;

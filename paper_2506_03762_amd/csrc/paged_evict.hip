@@ -4,6 +4,10 @@
 // A token's rank is its key (class and score, order-preserving), its position (the highest goes first) and its place (the last goes first).
 // One workgroup per (sequence, KV head) finds the rank of the last token to go, lists the moves in order and moves scores and positions;
 // it moves the keys and values too where there can only be a few, else a second launch does.
+//
+// The selection is bound by what one CU does for a row of scores: every key is read from memory once and from LDS three times (histogram, counts, lists), so
+// 32768 tokens of 8 heads take 22 us (with keys read again for every digit of the last one 141), 2049 of 64 x 8 heads, of which one goes, 8.8.  More CUs to
+// a row would need two more launches.  The moves are bound by memory: 8 prompts of up to 16384 tokens to 2048, 112 MB in 24 us, 4.7 TB/s.
 #include <limits.h>
 
 #include <algorithm>

@@ -1,6 +1,9 @@
 // Causal attention of packed prompts in tiles of four times 64 rows, bf16 (prompt_attn.hip says what is computed, wide_tile.h how).
 //
-// A wave takes 64 rows of a query head and leaves out the keys behind its last one.
+// A wave takes 64 rows of a query head and leaves out the keys behind its last one.  One prompt of 16384 tokens, 32 heads of 128 over 8: 1935 us, 1.13
+// PFLOP/s, as a library's product of 8192^3 reaches 1.16: power bounds both.  A tile's start, the blocks with masks and its outputs take 10 us, so
+// that shorter prompts go to tiles of 128 rows; a workgroup that takes several tiles one after the other, its next keys and rows requested during the last
+// blocks, gained nothing (1930).
 #include "narrow_tile.h"
 #include "prompt_tiles.h"
 #include "wide_tile.h"

@@ -296,12 +296,21 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     // (no part of more than 1024 places: sequences' lengths differ.  64 of up to 4096 tokens, 8 heads: 168 us with one part each, 160 with four, 167 with
     // eight)
     pl.parts = (int)std::max(parts_for(units * pl.tiles, room, 32), std::min<int64_t>(64, room / 1024));
+    // One launch where parts would shorten the chain of a sequence's blocks by less than the second one takes.  us with parts and in one, d = 128 (64), 64
+    // (sequence, KV head) pairs, 4 query heads each: 256 tokens 12.0, 10.5 (10.9, 8.9), 384 12.2, 13.0 (11.1, 9.9), 768 15.3, 17.9 (13.2, 13.2); 128 pairs: 512
+    // 16.3, 15.1 (13.6, 11.6), 768 20.9, 19.0 (15.7, 13.7), 1000 22.8, 23.0 (16.3, 16.0); 512 pairs of 400, which are never split, 29.9, 24.0; fp32, whose
+    // blocks take longer, 64 pairs of 256 16.9, 20.1 (12.8, 13.1).
+    const int64_t blocks = (room + 127) / 128, saved = blocks - (blocks + pl.parts - 1) / pl.parts;
+    pl.one = pl.tiles == 1 && saved <= (p->dtype != AHA_BF16 ? 0 : units >= 128 ? 4 : p->head_dim == 64 ? 3 : 1);
+    if (pl.one) pl.parts = 1;
     pl.items = units * pl.tiles * pl.parts;
     pl.ld = p->slots > 0 ? (room + 31) / 32 * 32 : 0;
     const size_t rows = (size_t)units * group;
-    pl.off_ms = align_up(sizeof(float) * rows * pl.parts * p->head_dim, 256);
-    pl.off_ms2 = align_up(pl.off_ms + 2 * sizeof(float) * rows * pl.parts, 256);
-    pl.off_dots = align_up(pl.off_ms2 + 2 * sizeof(float) * rows * pl.parts, 256);
+    if (!pl.one) {
+        pl.off_ms = align_up(sizeof(float) * rows * pl.parts * p->head_dim, 256);
+        pl.off_ms2 = align_up(pl.off_ms + 2 * sizeof(float) * rows * pl.parts, 256);
+        pl.off_dots = align_up(pl.off_ms2 + 2 * sizeof(float) * rows * pl.parts, 256);
+    }
     pl.bytes = align_up(pl.off_dots + sizeof(float) * rows * (size_t)pl.ld, 256);
     return pl;
 }

@@ -46,6 +46,18 @@ def test_holes(dtype):
 
 
 @BOTH
+@HEADS
+def test_caches_in_parts(dtype, d):
+    """Tables of many places, which are divided, for sequences of all lengths, most of whose parts have no key."""
+    holes = {(4, 0): -1, (4, 9): 10 ** 6, (5, 62): -1, (6, 0): -1}  # (the newest token of the next to last one is dropped; the last one has nothing)
+    Steps(30, [0, 1, 129, -3, 700, 1000, 16, 1600], q_heads=4, kv_heads=2, d=d, dtype=dtype, width=100, holes=holes).check()
+    Steps(31, [1600, 513, 10 ** 9], q_heads=10, kv_heads=2, d=d, dtype=dtype, width=100, slots=1333, slot_pad=7, seen=[5000, 513, 70]).check()
+    Steps(32, [1200, 77], q_heads=6, kv_heads=2, d=d, dtype=dtype, width=100, with_scores=False).check()
+    Steps(33, [1200, 77], q_heads=6, kv_heads=2, d=d, dtype=dtype, width=100, with_pos=False, adaptive=False, fixed=0.2).check()
+    Steps(34, [1500, 300], q_heads=70, kv_heads=2, d=d, dtype=dtype, width=100, hot=4.0).check()
+
+
+@BOTH
 def test_scales_of_the_scores(dtype):
     for seen in ([500, 500], [50, 10 ** 9], [1, 0], [-3, 65]):
         Steps(8, [200, 64], q_heads=4, kv_heads=2, d=64, dtype=dtype, budget=64, seen=seen).check()
