@@ -6,8 +6,9 @@
 // it moves the keys and values too where there can only be a few, else a second launch does.
 //
 // The selection is bound by what one CU does for a row of scores: every key is read from memory once and from LDS three times (histogram, counts, lists), so
-// 32768 tokens of 8 heads take 22 us (with keys read again for every digit of the last one 141), 2049 of 64 x 8 heads, of which one goes, 8.8.  More CUs to
-// a row would need two more launches.  The moves are bound by memory: 8 prompts of up to 16384 tokens to 2048, 112 MB in 24 us, 4.7 TB/s.
+// 32768 tokens of 8 heads take 22 us, 2049 of 64 x 8 heads, of which one goes, 8.8.  More CUs to a row would need two more launches.  Where the keys do not
+// fit, they are formed again from scores and positions in each of the four sweeps: 131072 tokens of 8 heads 118 us with the moves (digit by digit of the last
+// one's rank, twelve sweeps, 447).  The moves are bound by memory: 8 prompts of up to 16384 tokens to 2048, 112 MB in 24 us, 4.7 TB/s.
 #include <limits.h>
 
 #include <algorithm>
@@ -34,11 +35,12 @@ struct Rank {
 };
 __device__ __forceinline__ uint64_t rank_what(uint32_t key, int pos) { return (uint64_t)key << 32 | (uint32_t)~((uint32_t)pos ^ 0x80000000u); }
 
-constexpr int kEvictBins = 4096, kEvictCandidates = 1024;
+constexpr int kEvictCandidates = 1024;
 template <int WAVES>
 struct EvictLds {
+    static constexpr int kBins = WAVES * 256;  // four to a thread
     union {
-        int hist[kEvictBins];
+        alignas(16) int hist[kBins];
         Rank candidates[kEvictCandidates];
     };
     uint32_t all_low, all_above, from, to;
@@ -183,6 +185,63 @@ struct Eviction {
     }
 };
 
+// One histogram of the keys that may go, linear over their range: the bin of the last one to go, whose keys are then ranked against each other.
+template <int WAVES>
+struct EvictBins {
+    uint32_t low, slope;
+    // a little less than kBins 2^32 / (range + 1), which 64-bit division would take all waves 1.5 us for; 0: a bin for every key
+    __device__ __forceinline__ EvictBins(uint32_t low_, uint32_t above) : low(low_) {
+        constexpr int kBins = EvictLds<WAVES>::kBins;
+        const uint32_t range = above - 1 - low;
+        slope = range < kBins ? 0u : (uint32_t)(kBins * 0x1p32f * (1.f - 0x1p-20f) * __builtin_amdgcn_rcpf((float)range + 1.f));
+    }
+    __device__ __forceinline__ int bin_of(uint32_t k) const { return (int)(slope ? __umulhi(k - low, slope) : k - low); }
+    __device__ __forceinline__ uint64_t first_of(int bin) const {
+        return low + (slope ? (((uint64_t)bin << 32) + slope - 1) / slope : (uint64_t)bin);
+    }
+    // The bin that the last of `go` lies in: its keys are those from sm.from up to sm.to (smaller ones go, larger ones stay), sm.in_bin of them, of which
+    // number sm.rank from the smallest on is the last one.  All threads call it, between barriers of its own.
+    __device__ __forceinline__ void find(EvictLds<WAVES> &sm, int go, int tid) const {
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        __syncthreads();
+        const u32x4 c = *(const u32x4 *)&sm.hist[4 * tid];
+        const int sum = (int)((c[0] + c[1]) + (c[2] + c[3]));
+        int below = wave_prefix(sum, lane);
+        if (lane == 63) sm.count[1][wave] = below;
+        __syncthreads();
+        below -= sum;
+        for (int w = 0; w < wave; ++w) below += sm.count[1][w];
+        if (go > below && go <= below + sum) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (go > below && go <= below + (int)c[i]) sm.digit = tid * 4 + i, sm.rank = go - 1 - below, sm.in_bin = (int)c[i];
+                below += c[i];
+            }
+            sm.from = (uint32_t)first_of(sm.digit);
+            sm.to = (uint32_t)min(first_of(sm.digit + 1) - 1, (uint64_t)(kSafe - 1));
+        }
+        __syncthreads();
+    }
+};
+// The candidates, noted by all waves, ranked: sm.last is the last one to go, and what the waves have counted (sm.gaps, sm.movers; `per_wave` tokens to a wave)
+// is made complete.  Begins and ends with a barrier.
+template <int WAVES>
+__device__ __forceinline__ void rank_candidates(EvictLds<WAVES> &sm, int keep, int per_wave, int tid) {
+    const int in_bin = sm.in_bin, want = sm.rank;
+    __syncthreads();
+    for (int i = tid; i < in_bin; i += WAVES * 64) {
+        const Rank r = sm.candidates[i];
+        int smaller = 0;
+        for (int o = 0; o < in_bin; ++o) smaller += sm.candidates[o] < r;
+        if (smaller == want) sm.last = r;
+        // (what the rank says, too: the first want + 1 of them go)
+        const int j = (int)~r.place, w = j / per_wave;
+        if (smaller <= want && j < keep) atomicAdd(&sm.gaps[w], 1);
+        if (smaller > want && j >= keep) atomicAdd(&sm.movers[w], 1);
+    }
+    __syncthreads();
+}
+
 // The tokens' keys in LDS, `steps` steps of 64 tokens of a wave, one lane each, which alone reads them.  Returns the number of moves.
 // (`holes`: all threads call it; whether the sequence has one)
 template <int WAVES, class Holes>
@@ -264,7 +323,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
         free_keys = sm.all_free;
     };
     if (go > 1)
-        for (int i = tid; i < kEvictBins; i += THREADS) sm.hist[i] = 0;
+        *(u32x4 *)&sm.hist[4 * tid] = u32x4{0, 0, 0, 0};
     of_all();
     if (go > free_keys) {  // all that may go do, and protected ones by their position: other keys of the same order, positions in turns
         __syncthreads();
@@ -310,41 +369,15 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     int gaps = 0, movers = 0;
     bool found = false;
     {
-        // one histogram, linear over that range; the bin of the last one to go; its keys ranked against each other
-        const uint32_t range = above - 1 - low;
-        // (a little less than kEvictBins 2^32 / (range + 1), which 64-bit division would take all waves 1.5 us for)
-        const uint32_t slope = range < kEvictBins ? 0u : (uint32_t)(kEvictBins * 0x1p32f * (1.f - 0x1p-20f) * __builtin_amdgcn_rcpf((float)range + 1.f));
-        auto bin_of = [&](uint32_t k) { return (int)(slope ? __umulhi(k - low, slope) : k - low); };
+        const EvictBins<WAVES> bins(low, above);
 #pragma unroll 4
         for (int t = 0; t < steps; ++t) {
             const uint32_t k = key[t * 64];
-            if (k != kSafe) atomicAdd(&sm.hist[bin_of(k)], 1);
+            if (k != kSafe) atomicAdd(&sm.hist[bins.bin_of(k)], 1);
         }
-        __syncthreads();
-        constexpr int BPT = kEvictBins / THREADS;
-        int c[BPT], sum = 0;
-#pragma unroll
-        for (int i = 0; i < BPT; ++i) c[i] = sm.hist[tid * BPT + i], sum += c[i];
-        int below = wave_prefix(sum, lane);
-        if (lane == 63) sm.count[1][wave] = below;
-        __syncthreads();
-        below -= sum;
-        for (int w = 0; w < wave; ++w) below += sm.count[1][w];
-        if (go > below && go <= below + sum) {
-#pragma unroll
-            for (int i = 0; i < BPT; ++i) {
-                if (go > below && go <= below + c[i]) sm.digit = tid * BPT + i, sm.rank = go - 1 - below, sm.in_bin = c[i];
-                below += c[i];
-            }
-            // the bin's keys are those from `from` up to `to`; smaller ones go, larger ones stay
-            auto first_of = [&](int at) { return low + (slope ? (((uint64_t)at << 32) + slope - 1) / slope : (uint64_t)at); };
-            sm.from = (uint32_t)first_of(sm.digit);
-            sm.to = (uint32_t)min(first_of(sm.digit + 1) - 1, (uint64_t)(kSafe - 1));
-        }
-        __syncthreads();
-        const int in_bin = sm.in_bin, want = sm.rank;
+        bins.find(sm, go, tid);
         const uint32_t from = sm.from, to = sm.to;
-        if (in_bin <= kEvictCandidates) {
+        if (sm.in_bin <= kEvictCandidates) {
             found = true;
             auto note = [&](int t) {
                 const uint32_t k = key[t * 64];
@@ -368,18 +401,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
                 movers += __builtin_popcountll(stays);
             }
             if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
-            __syncthreads();
-            for (int i = tid; i < in_bin; i += THREADS) {
-                const Rank r = sm.candidates[i];
-                int smaller = 0;
-                for (int o = 0; o < in_bin; ++o) smaller += sm.candidates[o] < r;
-                if (smaller == want) sm.last = r;
-                // (what the rank says, too: the first want + 1 of them go)
-                const int j = (int)~r.place, w = j / per_wave;
-                if (smaller <= want && j < keep) atomicAdd(&sm.gaps[w], 1);
-                if (smaller > want && j >= keep) atomicAdd(&sm.movers[w], 1);
-            }
-            __syncthreads();
+            rank_candidates(sm, keep, per_wave, tid);
             last = sm.last;
         }
     }
@@ -430,38 +452,95 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     return moved;
 }
 
-// More tokens than that: keys are read again whenever they are needed.
-template <int WAVES>
-__device__ __forceinline__ int evict_from_memory(const Eviction &e, EvictLds<WAVES> &sm, int tid) {
-    constexpr int THREADS = WAVES * 64;
-    const int lane = tid & 63, wave = tid >> 6, len = e.len, keep = e.keep;
+// More tokens than that: their keys are formed again whenever they are needed.  `holes` as above; the moves' lists are `e.moves` themselves.
+template <int WAVES, class Holes>
+__device__ __forceinline__ int evict_from_memory(Eviction &e, EvictLds<WAVES> &sm, int tid, Holes holes) {
+    constexpr int THREADS = WAVES * 64, U = 8;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), len = e.len;
+    const int per_wave = (len + THREADS * U - 1) / (THREADS * U) * 64 * U, first = wave * per_wave, end = min(len, first + per_wave);
     const EvictRows &rows = e.rows;
-    const Rank last = last_to_go_by_digits(rows, len, len - keep, sm);
-    int gaps = 0, movers = 0;
-    for (int j0 = 0; j0 < len; j0 += THREADS) {
-        const int j = j0 + tid;
-        const bool there = j < len, goes = there && !(last < Rank{rank_what(rows.key_at(min(j, len - 1)), rows.pos_of(min(j, len - 1))), ~(uint32_t)j});
-        const bool gap = goes && j < keep, mover = there && !goes && j >= keep;
-        const uint64_t gm = __builtin_amdgcn_ballot_w64(gap), mm = __builtin_amdgcn_ballot_w64(mover);
-        __syncthreads();
-        if (lane == 0) sm.count[0][wave] = __builtin_popcountll(gm), sm.count[1][wave] = __builtin_popcountll(mm);
-        __syncthreads();
-        int before[2] = {gaps, movers};
-        for (int w = 0; w < WAVES; ++w) {
-            const int c0 = sm.count[0][w], c1 = sm.count[1][w];
-            if (w < wave) before[0] += c0, before[1] += c1;
-            gaps += c0;
-            movers += c1;
+    // work(j, key) for the wave's tokens, one per lane (behind the last token a protected one's); U steps' scores and positions are in flight
+    auto sweep = [&](auto work) {
+        for (int j0 = first + lane; j0 - lane < end; j0 += U * 64) {
+            float score[U];
+            int pos[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) score[u] = rows.scores[min(j0 + u * 64, len - 1)], pos[u] = rows.pos_of(min(j0 + u * 64, len - 1));
+#pragma unroll
+            for (int u = 0; u < U; ++u) work(j0 + u * 64, j0 + u * 64 < end ? rows.key_of(score[u], pos[u]) : kSafe, pos[u]);
         }
-        if (gap) e.moves[mask_number(gm, before[0])].x = j;
-        if (mover) e.moves[mask_number(mm, before[1])].y = j;
+    };
+    if (tid == 0) sm.all_low = kSafe, sm.all_above = 0, sm.all_free = 0, sm.n_candidates = 0;
+    *(u32x4 *)&sm.hist[4 * tid] = u32x4{0, 0, 0, 0};
+    uint32_t low = kSafe, above = 0;
+    int free_keys = 0;
+    sweep([&](int, uint32_t k, int) {
+        low = min(low, k);
+        above = max(above, k + 1);  // (0 of protected ones)
+        free_keys += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k != kSafe));
+    });
+    if (holes()) {  // (behind a barrier)
+        e.keep = len;
+        return 0;
     }
+    const int keep = e.keep, go = len - keep;
+    low = reduce_lanes<1, 64>(low, OpMinU{});
+    above = reduce_lanes<1, 64>(above, OpMaxU{});
+    if (lane == 0) atomicMin(&sm.all_low, low), atomicMax(&sm.all_above, above), atomicAdd(&sm.all_free, free_keys);
     __syncthreads();
-    for (int i = tid; i < gaps; i += THREADS) {
+    Rank last;
+    int gaps = 0, movers = 0;
+    bool found = false;
+    if (go <= sm.all_free) {
+        const EvictBins<WAVES> bins(sm.all_low, sm.all_above);
+        sweep([&](int, uint32_t k, int) {
+            if (k != kSafe) atomicAdd(&sm.hist[bins.bin_of(k)], 1);
+        });
+        bins.find(sm, go, tid);
+        const uint32_t from = sm.from, to = sm.to;
+        if (sm.in_bin <= kEvictCandidates) {
+            found = true;
+            sweep([&](int j, uint32_t k, int p) {
+                if (k >= from && k <= to) sm.candidates[atomicAdd(&sm.n_candidates, 1)] = Rank{rank_what(k, p), ~(uint32_t)j};
+                gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k < from && j < keep));
+                movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > to && j >= keep && j < end));
+            });
+            if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
+            rank_candidates(sm, keep, per_wave, tid);
+            last = sm.last;
+        }
+    }
+    auto goes = [&](int j, uint32_t k, int p) { return !(last < Rank{rank_what(k, p), ~(uint32_t)j}); };
+    if (!found) {  // more protected tokens go, or too many keys are alike
+        last = last_to_go_by_digits(rows, len, go, sm);
+        sweep([&](int j, uint32_t k, int p) {
+            const bool out = goes(j, k, p);
+            gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(out && j < min(keep, end)));
+            movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!out && j >= keep && j < end));
+        });
+        if (lane == 0) sm.gaps[wave] = gaps, sm.movers[wave] = movers;
+        __syncthreads();
+    }
+    gaps = movers = 0;
+    int moved = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        moved += sm.gaps[w];  // (as many as movers)
+        if (w < wave) gaps += sm.gaps[w], movers += sm.movers[w];
+    }
+    sweep([&](int j, uint32_t k, int p) {
+        const bool out = goes(j, k, p), gap = out && j < min(keep, end), mover = !out && j >= keep && j < end;
+        const uint64_t gm = __builtin_amdgcn_ballot_w64(gap), mm = __builtin_amdgcn_ballot_w64(mover);
+        if (gap) e.moves[mask_number(gm, gaps)].x = j;
+        if (mover) e.moves[mask_number(mm, movers)].y = j;
+        gaps += __builtin_popcountll(gm);
+        movers += __builtin_popcountll(mm);
+    });
+    __syncthreads();
+    for (int i = tid; i < moved; i += THREADS) {
         const int2 mv = e.moves[i];
         e.move(i, mv.x, mv.y);
     }
-    return gaps;  // (as many as movers)
+    return moved;
 }
 
 // Dynamic LDS: the keys of pl.lds_tokens tokens (and of the places behind the last), then the places that become free and those that
@@ -495,10 +574,8 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictGeom g, E
         e.copy(tid, THREADS);
     } else if (e.len <= pl.lds_tokens) {
         moved = evict_in_lds<WAVES>(e, sm, dynamic, (uint16_t *)(dynamic + (pl.lds_tokens + THREADS)), tid, holes);
-    } else if (holes()) {
-        e.keep = e.len;
-    } else {
-        moved = evict_from_memory(e, sm, tid);
+    } else if constexpr (WAVES == 16) {  // (fewer waves are for so few tokens that all keys fit)
+        moved = evict_from_memory(e, sm, tid, holes);
     }
     if (e.keep > g.budget) e.copy(tid, THREADS);  // (a hole: all places)
     if (tid == 0) {

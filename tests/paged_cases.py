@@ -289,7 +289,8 @@ class Evictions(Caches):
                         return (2, 0.0, -at[j], -j)
                     return (0, 0.0, -at[j], -j) if sc[j] != sc[j] else (1, sc[j], -at[j], -j)
                 stay = sorted(sorted(range(n), key=worth)[n - keep:])
-                free = [j for j in range(keep) if j not in set(stay)]
+                kept = set(stay)
+                free = [j for j in range(keep) if j not in kept]
                 source = list(range(keep))
                 for to, frm in zip(free, [j for j in stay if j >= keep]):
                     source[to] = frm

@@ -114,6 +114,19 @@ def test_few_long_sequences_among_many():
         assert torch.equal(d[name].view(torch.uint8), want[name].view(torch.uint8)), name
 
 
+@PLACE
+def test_long_sequences_of_any_kind(in_place):
+    """Ties, infinities, NaN, most tokens protected, pages that are not there, one token and nearly all that go."""
+    n = 40000
+    rng = np.random.default_rng(11)
+    tied = torch.from_numpy(rng.choice(np.array([0.0, -0.0, 2.0, np.nan, np.inf, -1.0], np.float32), (1, 2, n)))
+    pos = torch.from_numpy(rng.permuted(np.tile(np.arange(n), (1, 2, 1)), axis=2).astype(np.int32))
+    for budget, recent in ((n - 1, 0), (n - 300, 20000), (5, 3), (12000, 12000)):
+        Evictions(21, [n], kv_heads=2, d=64, budget=budget, recent=recent, scores=tied, pos=pos, page=64, slots=n, seen=[n + 5000], in_place=in_place).check()
+    Evictions(22, [n], kv_heads=2, d=64, budget=15000, recent=15000, seen=[0], page=64, slots=n, in_place=in_place).check()
+    Evictions(23, [n, 36000], kv_heads=1, d=64, budget=900, page=64, holes={(1, 300): -1}, in_place=in_place).check()
+
+
 def test_shared_scores():
     """One row of scores for all heads, expanded, into outputs of their own."""
     base = torch.rand(2, 1, 160, generator=torch.Generator().manual_seed(1))
