@@ -134,7 +134,8 @@ __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf
 }
 
 // The dots of 32 keys and 32 rows in four chains of D / 4 products: eight, as in f32_tile.h, leave no room beside the outputs (d = 128, 8
-// sequences of one prefix of 2048 keys 26.3 us, so 21.6; 2 x 64 rows x 4 heads, 4096 keys 57.4, 49.5; d = 64 37.2, 29.0).
+// sequences of one prefix of 2048 keys 26.3 us, so 21.6; 2 x 64 rows x 4 heads, 4096 keys 57.4, 49.5, d = 64 37.2, 29.0, which are 28.9 and 21.1 with loads
+// ahead).
 template <int D>
 __device__ __forceinline__ f32x16 dots_f32(const f32x4 (&a)[D / 8], const float *sq) {
     f32x16 acc[4];
