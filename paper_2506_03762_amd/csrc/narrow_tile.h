@@ -153,7 +153,8 @@ __device__ __forceinline__ f32x16 dots_f32(const f32x4 (&a)[D / 8], const float 
     for (int v = 0; v < 16; ++v) acc[0][v] = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
     return acc[0];
 }
-// fp32: v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it beyond a few blocks' latency); a lane's chunks of a key row and a query row as in f32_tile.h (`sq`: its row in LDS, from its half's first chunk on);
+// fp32: v_mfma_f32_32x32x2_f32 (256 operations per CU and cycle, which bound it beyond a few blocks' latency); a lane's chunks of a key row and a query
+// row as in f32_tile.h (`sq`: its row in LDS, from its half's first chunk on);
 // the second product takes the weights from the accumulators one element at a time, a contraction step over the keys of the
 // two half-waves, and a value row's 32 channels per load straight from memory.  With nothing requested ahead a prompt of 512 tokens, 2 heads of 64, took
 // 21.8 us, so 15.3.

@@ -8,8 +8,8 @@
 // workgroup does that itself (plan_paged() says when).
 //
 // Bound by memory: keys and values are read once, for all query heads of their KV head, and two operations per element and head are far below what the
-// matrix core gives.  64 caches of up to 4096 tokens, 8 heads of 128: 670 MB in 145 us, 4.6 TB/s (a copy reaches 4.95), joining 12 more; one cache of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.6 + 4.5, of which 14 are the
-// 67 MB.  Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
+// matrix core gives.  64 caches of up to 4096 tokens, 8 heads of 128: 670 MB in 145 us, 4.6 TB/s (a copy reaches 4.95), joining 12 more; one cache
+// of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.5 + 4.5, of which 14 are the 67 MB.  Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
 #include <limits.h>
 
 #include "narrow_tile.h"

@@ -417,7 +417,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
         last = last_to_go_by_digits(rows, len, go, sm);
         last_key = 0;
         for (int t = 0; t < steps; ++t)
-            if (base + t * 64 < len) key[t * 64] = last < Rank{rank_what(rows.key_at(base + t * 64), rows.pos_of(base + t * 64)), ~(uint32_t)(base + t * 64)} ? kSafe : 0u;
+            if (base + t * 64 < len) key[t * 64] = last < rank_of(t, rows.key_at(base + t * 64)) ? kSafe : 0u;
         for (int t = 0; t < front_steps; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[t * 64] == 0 && base + t * 64 < keep));
         for (int t = back; t < steps; ++t)
             movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[t * 64] != 0 && (uint32_t)(base + t * 64 - keep) < (uint32_t)go));

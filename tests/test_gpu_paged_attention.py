@@ -97,9 +97,10 @@ def test_the_newest_token_starts_from_nothing():
 
 
 @BOTH
-def test_keys_and_values_that_are_not_finite(dtype):
+@pytest.mark.parametrize("width", [None, 100])
+def test_keys_and_values_that_are_not_finite(dtype, width):
     """They reach their own sequence and KV head alone."""
-    c = Steps(20, [300, 200], q_heads=4, kv_heads=2, d=64, dtype=dtype)
+    c = Steps(20, [300, 200], q_heads=4, kv_heads=2, d=64, dtype=dtype, width=width)
     d = c.upload()
     c.run(d)
     torch.cuda.synchronize()

@@ -111,3 +111,20 @@ def test_captured_prompts_follow_their_lengths():
         d["lse"].fill_(NAN)
         graph.replay()
         c.check(d)
+
+
+def test_far_strides():
+    """Rows whose offsets pass 2^31 elements."""
+    n, d = 2100, 128
+    c = wide(15, [n], d, group=1)
+    step = 2 ** 31 // 2000 // 8 * 8 + 1024
+    base = torch.empty(n * step, dtype=torch.bfloat16, device="cuda")
+    dev = c.upload()
+    for i, name in enumerate(("q", "k", "v", "out")):
+        far = base.as_strided((n, c.hq, d), (step, d, 1), c.hq * d * i)
+        far.copy_(dev[name])
+        dev[name] = far
+    from paper_2506_03762_amd import binding as B
+    dev["p"] = B.PromptAttention.of(dev["q"], dev["k"], dev["v"], dev["out"], dev["first"], c.scale)
+    c.run(dev)
+    c.check(dev)
