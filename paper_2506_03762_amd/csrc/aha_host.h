@@ -300,7 +300,7 @@ struct PromptGeom {
     float c_out;  // scale times log2(e), above 0
 };
 struct PromptPlan {
-    int rows;       // of a tile: 32, 128 (prompt_mid.hip) or 256 (prompt_wide.hip)
+    int rows;       // of a tile: 16 (fp32), 32, 128 (prompt_mid.hip) or 256 (prompt_wide.hip)
     int64_t items;  // workgroups, at most (the prompts' lengths are known on the device)
 };
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
@@ -325,7 +325,8 @@ struct PagedGeom {
     float c_out, fixed_scale, lambda_floor;  // c_out: scale times log2(e), above 0
 };
 struct PagedPlan {
-    int tiles, parts;   // of 32 rows of a (sequence, KV head), of its keys
+    int rows;           // of a tile: 32, or 16 (fp32)
+    int tiles, parts;   // of the rows of a (sequence, KV head), of its keys
     bool one;           // launch: there is one part, and one tile
     int64_t items, ld;  // workgroups; floats of a row of dots
     size_t off_ms, off_ms2, off_dots, bytes;  // behind the partial outputs: references and sums, of the output's weights and of the scores'

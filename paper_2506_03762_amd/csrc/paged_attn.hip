@@ -12,7 +12,7 @@
 // of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.5 + 4.5, of which 14 are the 67 MB.  Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
 #include <limits.h>
 
-#include "narrow_tile.h"
+#include "small_tile.h"
 
 namespace aha {
 
@@ -82,16 +82,17 @@ struct ScoreLoads {
 __device__ __forceinline__ float2 score_norm(float ref, float all) { return make_float2(ref, all > 0.f ? 1.f / all : all == 0.f ? 0.f : all); }
 
 // ONE: all keys are one part, whose outputs and scores are formed here.
-template <class T, int D, bool ONE>
+template <class T, int D, int ROWS, bool ONE>
 __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_kernel(PagedGeom g, PagedPlan pl, float *part_o, float2 *part_ms,
                                                                               float2 *part_ms2, float *dots) {
+    using A = Tile<T, D, ROWS>;
     constexpr int STEP = NarrowRows<D>::STEP;
-    __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<T, D>()];
-    __shared__ float2 s_ms2[4][32], s_norm[32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    __shared__ __attribute__((aligned(1024))) char smem[A::lds];
+    __shared__ float2 s_ms2[4][ROWS], s_norm[ROWS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane % ROWS;
     // (sequence, KV head) by part by tile
     const int id = blockIdx.x, tile = id % pl.tiles, part = id / pl.tiles % pl.parts, z = id / pl.tiles / pl.parts;
-    const int b = z / g.Hkv, h = z % g.Hkv, row0 = tile * 32, rows = min(32, g.G - row0);
+    const int b = z / g.Hkv, h = z % g.Hkv, row0 = tile * ROWS, rows = min(ROWS, g.G - row0);
     const int len = uniform(tokens_of(g, b)), steps = (len + STEP - 1) / STEP;
     const bool live = col < rows;
     const int gi = row0 + min(col, rows - 1), hq = h * g.G + gi;
@@ -111,48 +112,56 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void paged_part_ker
         return;
     }
     const T *q = (const T *)g.q + b * g.qs[0] + hq * g.qs[1];
-    float *to = dots + ((int64_t)b * g.Hq + hq) * pl.ld + 4 * hf;
+    float *to = dots + ((int64_t)b * g.Hq + hq) * pl.ld + A::first(lane);
     const float lam = dots ? score_scale(g, b) : 0.f;
     float m2 = -INFINITY, s2 = 0.f;
-    auto block = [&](int kb, const f32x16 &acc) {
+    auto block = [&](int kb, const auto &acc) {
         if (!dots) return;
         if (live) {
 #pragma unroll
-            for (int v = 0; v < 16; v += 4) *(f32x4 *)(to + kb + 2 * v) = f32x4{acc[v], acc[v + 1], acc[v + 2], acc[v + 3]};
+            for (int v = 0; v < A::N; v += 4) *(f32x4 *)(to + kb + A::key(v)) = f32x4{acc[v], acc[v + 1], acc[v + 2], acc[v + 3]};
         }
         float top = -INFINITY;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[v]);
+        for (int v = 0; v < A::N; ++v) top = fmaxf(top, acc[v]);
         const float mn = fmaxf(m2, top * lam), ref = mn == -INFINITY ? 0.f : mn;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sum[v & 3] += fast_exp2(fmaf(acc[v], lam, -ref));
+        for (int v = 0; v < A::N; ++v) sum[v & 3] += fast_exp2(fmaf(acc[v], lam, -ref));
         s2 = s2 * fast_exp2(m2 - ref) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
         m2 = mn;
     };
-    f32x16 O[D / 32];
+    typename A::Out O;
     float m, s;
     no_rows_yet(O, m, s);
     if constexpr (sizeof(T) == 2) {
         bf16x8 qf[D / 16];
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-            qf[ks] = *(const bf16x8 *)(q + hf * 8 + ks * 16);
+            qf[ks] = *(const bf16x8 *)(q + (lane >> 5) * 8 + ks * 16);
             if (!live) qf[ks] = bf16x8{};
         }
         narrow_sweep<D, true>(keys, qf, INT_MAX, g.c_out, smem, lane, wave, O, m, s, block);
+    } else if constexpr (ROWS == 16) {
+        f32x4 qf[D / 16];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            qf[i] = *(const f32x4 *)(q + A::first(lane) + 16 * i);
+            if (!live) qf[i] = f32x4{};
+        }
+        f32_sweep16<D>(keys, qf, INT_MAX, g.c_out, lane, wave, O, m, s, block);
     } else {
         float *sQ = (float *)smem;
         stage_f32_rows<D>(sQ, q, live, lane, wave);
         __syncthreads();
-        f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, INT_MAX, g.c_out, lane, wave, O, m, s, block);
+        f32_sweep<D>(keys, sQ + col * f32_ld(D) + A::first(lane), INT_MAX, g.c_out, lane, wave, O, m, s, block);
     }
-    if (dots) {  // the sums of the half-waves, later those of the waves
-        const float M = combine_lane_xor<32>(m2, OpMax{}), ref = M == -INFINITY ? 0.f : M;
-        const float all = combine_lane_xor<32>(s2 * fast_exp2(m2 - ref), OpSum{});
-        if (lane < 32) s_ms2[wave][lane] = make_float2(M, all);
+    if (dots) {  // the sums of a row's lanes, later those of the waves
+        const float M = reduce_lanes<ROWS, 64>(m2, OpMax{}), ref = M == -INFINITY ? 0.f : M;
+        const float all = reduce_lanes<ROWS, 64>(s2 * fast_exp2(m2 - ref), OpSum{});
+        if (lane < ROWS) s_ms2[wave][lane] = make_float2(M, all);
     }
-    const float *sums = (const float *)(smem + WaveMerge<D>::off_sums);
+    const float *sums = (const float *)(smem + A::off_sums);
     meet_waves<D>(
         rows, live, O, m, s, smem, lane, wave,
         [&](float M, float all) {
@@ -251,17 +260,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedGeom g, PagedPlan 
     l.add(g, x, pl.ld, F, g.pos ? g.pos + b * g.ps[0] + h * g.ps[1] : nullptr, at, j0, len, seen, score_scale(g, b), norm);
 }
 
+template <class T, int D, int ROWS>
+static hipError_t launch_parts(const PagedGeom &g, const PagedPlan &pl, float *part_o, float2 *part_ms, float2 *part_ms2, float *dots, hipStream_t st) {
+    if (pl.one) hipLaunchKernelGGL((paged_part_kernel<T, D, ROWS, true>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
+    else hipLaunchKernelGGL((paged_part_kernel<T, D, ROWS, false>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
+    return hipGetLastError();
+}
 template <class T, int D>
 static hipError_t launch_paged_t(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st) {
     float *part_o = (float *)ws, *dots = g.slots > 0 ? (float *)((char *)ws + pl.off_dots) : nullptr;
     float2 *part_ms = (float2 *)((char *)ws + pl.off_ms), *part_ms2 = (float2 *)((char *)ws + pl.off_ms2);
-    if (pl.one) {
-        hipLaunchKernelGGL((paged_part_kernel<T, D, true>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL((paged_part_kernel<T, D, false>), dim3((unsigned)pl.items), dim3(256), 0, st, g, pl, part_o, part_ms, part_ms2, dots);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    hipError_t e;
+    if constexpr (sizeof(T) == 4) e = pl.rows == 16 ? launch_parts<T, D, 16>(g, pl, part_o, part_ms, part_ms2, dots, st) : launch_parts<T, D, 32>(g, pl, part_o, part_ms, part_ms2, dots, st);
+    else e = launch_parts<T, D, 32>(g, pl, part_o, part_ms, part_ms2, dots, st);
+    if (e != hipSuccess || pl.one) return e;
     const int score_wgs = g.slots > 0 ? (int)((pl.ld + kJoinKeys - 1) / kJoinKeys) : 0;
     auto join = [&](auto kernel, int rows) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)((g.G + rows - 1) / rows + score_wgs), g.batch * g.Hkv), dim3(256), 0, st, g, pl, part_o, part_ms,

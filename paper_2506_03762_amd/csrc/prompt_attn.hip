@@ -13,16 +13,17 @@
 
 #include "narrow_tile.h"
 #include "prompt_tiles.h"
+#include "small_tile.h"
 
 namespace aha {
 
-// ---- tiles of 32 rows ----
-template <class T, int D>
+template <class T, int D, int ROWS>
 __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_kernel(PromptGeom g) {
-    __shared__ __attribute__((aligned(1024))) char smem[narrow_lds<T, D>()];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
+    using A = Tile<T, D, ROWS>;
+    __shared__ __attribute__((aligned(1024))) char smem[A::lds];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane % ROWS;
     PromptTile it;
-    if (!prompt_tile(g, 32, (int)blockIdx.x, lane, it)) return;
+    if (!prompt_tile(g, ROWS, (int)blockIdx.x, lane, it)) return;
     KeyPlaces<T> keys;
     keys.in_a_row((const T *)g.k + it.lo * g.ks[0] + it.h * g.ks[1], (const T *)g.v + it.lo * g.vs[0] + it.h * g.vs[1], g.ks[0], g.vs[0]);
     keys.begin = 0;
@@ -30,21 +31,26 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
     const bool live = it.row0 + col < it.row1;
     const int token = min(it.row0 + col, it.row1 - 1), limit = token - it.lo;
     const T *q = (const T *)g.q + token * g.qs[0] + it.hq * g.qs[1];
-    f32x16 O[D / 32];
+    typename A::Out O;
     float m, s;
     no_rows_yet(O, m, s);
     if constexpr (sizeof(T) == 2) {
         bf16x8 qf[D / 16];
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + hf * 8 + ks * 16);
+        for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + (lane >> 5) * 8 + ks * 16);
         narrow_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s, [](int, const f32x16 &) {});
+    } else if constexpr (ROWS == 16) {
+        f32x4 qf[D / 16];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) qf[i] = *(const f32x4 *)(q + A::first(lane) + 16 * i);
+        f32_sweep16<D>(keys, qf, limit, g.c_out, lane, wave, O, m, s, [](int, const f32x8 &) {});
     } else {
         float *sQ = (float *)smem;
         stage_f32_rows<D>(sQ, q, true, lane, wave);
         __syncthreads();
-        f32_sweep<D>(keys, sQ + col * f32_ld(D) + 4 * hf, limit, g.c_out, lane, wave, O, m, s, [](int, const f32x16 &) {});
+        f32_sweep<D>(keys, sQ + col * f32_ld(D) + A::first(lane), limit, g.c_out, lane, wave, O, m, s, [](int, const f32x16 &) {});
     }
-    const float *sums = (const float *)(smem + WaveMerge<D>::off_sums);
+    const float *sums = (const float *)(smem + A::off_sums);
     meet_waves<D>(
         it.row1 - it.row0, live, O, m, s, smem, lane, wave,
         [&](float M, float all) {
@@ -55,17 +61,18 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
         });
 }
 
-template <class T>
+template <class T, int ROWS>
 static hipError_t launch_prompt_t(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
-    if (g.d == 64) hipLaunchKernelGGL((prompt_narrow_kernel<T, 64>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((prompt_narrow_kernel<T, 128>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
+    if (g.d == 64) hipLaunchKernelGGL((prompt_narrow_kernel<T, 64, ROWS>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((prompt_narrow_kernel<T, 128, ROWS>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
     return hipGetLastError();
 }
 
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
     if (pl.rows == 128) return launch_prompt_mid(g, pl, st);
     if (pl.rows > 32) return launch_prompt_wide(g, pl, st);
-    return g.dtype == AHA_BF16 ? launch_prompt_t<__bf16>(g, pl, st) : launch_prompt_t<float>(g, pl, st);
+    if (g.dtype == AHA_BF16) return launch_prompt_t<__bf16, 32>(g, pl, st);
+    return pl.rows == 16 ? launch_prompt_t<float, 16>(g, pl, st) : launch_prompt_t<float, 32>(g, pl, st);
 }
 
 }  // namespace aha

@@ -226,24 +226,31 @@ static PromptPlan plan_prompt(const aha_prompt *p) {
     // the table).  d = 128, 32 heads over 8: one prompt of 512 14.8, 17.0, 21.7, 1024 36, 29.3, 34.9, 4096 310, 158, 138, 16 of 200 55, 24.7, 32;
     // 8 over 2: one of 2048 36.6, 49.4, 59, 16 of 64 7.6, 7.1, 10.3.  d = 64, 16 heads: one of 1024 13.8, 21.8, 28.4, of 4096 94, 80, 88, 16 of
     // 500 49, 29.3, 28.9.
+    // fp32, 300 shapes: 1.0 and 0.6 % (1.15 and 1.4 times: 16 prompts of 20 tokens, 16 heads, 8.0, 10.9 in the order of the table).  d = 64: one prompt of 512, 2
+    // heads, 10.7, 16.0, 8 heads of 2048 71, 69, of 4096 245, 191; d = 128: 2 heads of 1024 28.9, 43.9, 8 of 1024 56, 47.
     static constexpr PromptTiles kTiles[2][3] = {
         {{32, 32, 512, 5.94f, .235f, 1.f}, {128, 32, 512, 5.38f, .49f, 1.26f}, {256, 64, 256, 5.81f, .55f, 1.f}},    // d = 64
         {{32, 32, 512, 8.9f, .4125f, 1.f}, {128, 32, 512, 8.2f, .66f, 1.3f}, {256, 64, 256, 13.4f, .66f, 1.f}}};  // d = 128
     const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads, n = (p->tokens + prompts - 1) / prompts;
+    static constexpr PromptTiles kTilesF32[2][2] = {{{16, 16, 256, 4.11f, .6f, .48f}, {32, 32, 256, 6.55f, .72f, .68f}},    // d = 64
+                                                    {{16, 16, 256, 5.41f, 1.18f, .67f}, {32, 32, 256, 9.29f, 1.15f, .73f}}};  // d = 128
     float least = INFINITY;
-    for (const PromptTiles &t : kTiles[p->head_dim == 128]) {
-        if (t.rows > 32 && p->dtype != AHA_BF16) continue;
+    auto try_tiles = [&](const PromptTiles &t) {
         const int64_t units = (n + t.unit - 1) / t.unit * group, heads = t.rows / t.unit;  // (a tile of 32 rows: one unit)
         const int64_t tiles = prompts * ((units + heads - 1) / heads) * p->n_kv_heads;
         const float keys = t.block * (float)n / 32;
         const float time = t.start + keys + std::max(0.f, (float)tiles / t.slots - 1.f) * t.later * (t.start + keys / 2);
-        if (time >= least) continue;
+        if (time >= least) return;
         least = time;
         pl.rows = t.rows;
         // at most: one unit's rows, and one tile, of every prompt are not full
         pl.items = ((p->tokens + (t.unit - 1) * prompts) / t.unit * group + prompts * (heads - 1)) / heads * p->n_kv_heads;
         if (heads == 1) pl.items = (pl.items / group + 7) / 8 * 8 * group;
-    }
+    };
+    if (p->dtype == AHA_BF16)
+        for (const PromptTiles &t : kTiles[p->head_dim == 128]) try_tiles(t);
+    else
+        for (const PromptTiles &t : kTilesF32[p->head_dim == 128]) try_tiles(t);
     return pl;
 }
 
@@ -292,7 +299,10 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     const int64_t units = (int64_t)p->batch * p->n_kv_heads;
     int64_t room = (int64_t)pages->table_width * pages->page_size;
     if (p->slots > 0) room = std::min<int64_t>(room, p->slots);
-    pl.tiles = (group + 31) / 32;
+    // (fp32: tiles of 32 rows that are half empty take 1.2 to 1.5 times as long: d = 128 (64), 8 caches of 400 tokens, 8 x 4 heads 19.5, so 15.4 us (13.1, 11.3),
+    // 64 of 1000, 8 x 1 heads 130, 107 (59, 47))
+    pl.rows = p->dtype == AHA_F32 && group <= 16 ? 16 : 32;
+    pl.tiles = (group + pl.rows - 1) / pl.rows;
     // (no part of more than 1024 places: sequences' lengths differ.  64 of up to 4096 tokens, 8 heads: 168 us with one part each, 160 with four, 167 with
     // eight)
     pl.parts = (int)std::max(parts_for(units * pl.tiles, room, 32), std::min<int64_t>(64, room / 1024));
