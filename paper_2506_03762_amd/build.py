@@ -1,14 +1,16 @@
-"""Build libaha.so (the gfx950 kernels and their C ABI) in-tree with hipcc."""
+"""Build libaha.so (the gfx950 kernels and their C ABI) in-tree with hipcc, and the binding's look at its tensors with g++."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaha.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["aha_api.hip", "value_prior.hip", "score_f32.hip", "score_hold_f32.hip", "score_bf16.hip", "score_full.hip", "score_window.hip", "score_share.hip", "score_given.hip",
@@ -30,6 +32,21 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
+def build_tensors() -> None:
+    """Compile the Python module that checks a call's tensors against their description."""
+    import torch
+    from torch.utils import cpp_extension
+    include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
+    tmp = TENSORS + ".tmp.%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           *("-isystem" + p for p in include), os.path.join(CSRC, "tensors.cpp"), "-o", tmp,
+           *("-L" + p for p in cpp_extension.library_paths()), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on tensors.cpp:\n%s" % r.stderr[-6000:])
+    os.replace(tmp, TENSORS)
+
+
 def build(verbose: bool = False, jobs: int = 8) -> str:
     """Compile every kernel source for gfx950 and link libaha.so. Always compiles."""
     os.makedirs(OBJDIR, exist_ok=True)
@@ -46,7 +63,9 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=jobs) as ex:
+        tensors = ex.submit(build_tensors)
         objs = list(ex.map(compile_one, SOURCES))
+        tensors.result()
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [cc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs,
            "-Wl,--version-script=" + os.path.join(CSRC, "aha.map")]

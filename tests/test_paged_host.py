@@ -183,3 +183,18 @@ def test_descriptions_refuse_other_layouts():
     for bad in ((scores[:1], None, scores, pos), (scores, None, scores[..., :9], pos), (scores, pos, scores, pos[:, :1]), (scores, None, pos, pos)):
         with pytest.raises(ValueError):
             B.PagedEviction.of(*bad, cache, budget=64)
+
+
+def test_tensors_in_one_look():
+    """The compiled checks of a call's tensors say the same as those that name what is wrong."""
+    from paper_2506_03762_amd import _tensors
+    rows, few = torch.zeros(4, 6, 8, dtype=torch.bfloat16)[:, ::2], torch.zeros(5, dtype=torch.int32)
+    what = (("q", torch.bfloat16, None, rows.shape, rows.stride()), ("seen", torch.int32, 5, None, None), ("pos", torch.int32, None, (), ()))
+    assert _tensors.pointers(what, (rows, few, None), -1) == [rows.data_ptr(), few.data_ptr(), None]
+    assert B._fast_pointers is _tensors.pointers
+    for given, device in (((rows, few, None), 0), ((rows.float(), few, None), -1), ((rows.contiguous(), few, None), -1), ((rows[:3], few, None), -1),
+                          ((rows, few[:4], None), -1), ((rows, torch.zeros(10, dtype=torch.int32)[::2], None), -1), ((rows, few.long(), None), -1),
+                          ((rows, few, few), -1), ((rows, few), -1), ((rows, 5, None), -1), ((rows, few.to_sparse(), None), -1),
+                          ((rows, few.numpy(), None), -1)):
+        assert _tensors.pointers(what, given, device) is None, given
+    assert _tensors.pointers((("x",),), (few,), -1) is None and _tensors.pointers(what, (rows, few, None)) is None
