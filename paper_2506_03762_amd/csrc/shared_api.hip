@@ -309,9 +309,11 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     // One launch where parts would shorten the chain of a sequence's blocks by less than the second one takes.  us with parts and in one, d = 128 (64), 64
     // (sequence, KV head) pairs, 4 query heads each: 256 tokens 12.0, 10.5 (10.9, 8.9), 384 12.2, 13.0 (11.1, 9.9), 768 15.3, 17.9 (13.2, 13.2); 128 pairs: 512
     // 16.3, 15.1 (13.6, 11.6), 768 20.9, 19.0 (15.7, 13.7), 1000 22.8, 23.0 (16.3, 16.0); 512 pairs of 400, which are never split, 29.9, 24.0; fp32, whose
-    // blocks take longer, 64 pairs of 256 16.9, 20.1 (12.8, 13.1).
+    // blocks take longer, 64 pairs of 256 13.8, 14.3 (11.3, 10.2), 128 pairs of 768 31.8, 28.9 (21.5, 19.2), in tiles of 32 rows 64 pairs of 256 16.9, 20.1 (12.8,
+    // 13.1).
     const int64_t blocks = (room + 127) / 128, saved = blocks - (blocks + pl.parts - 1) / pl.parts;
-    pl.one = pl.tiles == 1 && saved <= (p->dtype != AHA_BF16 ? 0 : units >= 128 ? 4 : p->head_dim == 64 ? 3 : 1);
+    const bool bf16 = p->dtype == AHA_BF16;
+    pl.one = pl.tiles == 1 && saved <= (!bf16 && pl.rows > 16 ? 0 : units >= 128 ? 4 : p->head_dim == 64 ? (bf16 ? 3 : 1) : (bf16 ? 1 : 0));
     if (pl.one) pl.parts = 1;
     pl.items = units * pl.tiles * pl.parts;
     pl.ld = p->slots > 0 ? (room + 31) / 32 * 32 : 0;
