@@ -3,12 +3,13 @@
 //   out_t = sum_{j <= t} softmax_j(scale q_t . K_j) V_j,   j in t's prompt
 //
 // in one pass over a row's keys with a running reference m.  A workgroup takes a tile of rows and all keys up to its last one, so that nothing has to be
-// joined and a call is one launch.  Tiles have 32 rows (here; narrow_tile.h), 128 (prompt_mid.hip) or 256 (prompt_wide.hip); plan_prompt() chooses.
+// joined and a call is one launch.  Tiles have 32 rows (here; narrow_tile.h), fp32 also 16 (small_tile.h), 128 (prompt_mid.hip) or 256 (prompt_wide.hip);
+// plan_prompt() chooses.
 //
 // Here four waves divide the keys of 32 rows of one head: the shortest chain for few rows, bound by the latency of its blocks of 128 keys (d = 64 0.9 us, of
 // which the loads are requested one block ahead; 128 1.65 us), but every tile reads its keys and values from the L2 again.  9 prompts of up to 777 tokens, 6 heads of
-// 64 over 2: 12.6 us.  fp32 has no other tiles: one prompt of 512, 2 heads of 64, 15.2 us, 32 tiles on as many CUs, each bound by the fp32 products of
-// its rows; with eight waves to a tile every shape was slower.
+// 64 over 2: 12.6 us.  fp32: one prompt of 512, 2 heads of 64, 9.9 us in 64 tiles of 16 rows, 15.2 in 32 of 32, each bound by the products of its rows; of
+// 4096, 32 heads of 128 over 8, 1276 us, 108 TFLOP/s, 0.70 of a library's product of 8192^3.  With eight waves to a tile every shape was slower.
 #include <limits.h>
 
 #include "narrow_tile.h"
