@@ -48,6 +48,15 @@ def test_many_prompts(count):
     Prompts(9, lens, q_heads=2, kv_heads=1, d=64).check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_problems_that_fill_the_chip(d):
+    """Few rows go to tiles of 16, these to tiles of 32."""
+    for seed, lens, group, more in ((40, [2049], 4, {}), (41, [1500, 1, 0, 2200], 3, dict(layout="htd", gap=5)), (42, [1900, 2100], 1, dict(hot=4.0, pad=4)),
+                                    (43, [31, 33, 2500, 1800], 2, dict(scale=0.7))):
+        heads = 36 // group * group
+        Prompts(seed, lens, q_heads=heads, kv_heads=heads // group, d=d, dtype=torch.float32, heads=[0, group - 1, heads - 1], **more).check()
+
+
 @BOTH
 def test_scales_and_large_logits(dtype):
     Prompts(10, [200, 33], q_heads=2, kv_heads=1, d=128, dtype=dtype, scale=0.0).check()
