@@ -14,7 +14,8 @@ __device__ __forceinline__ int prompt_of(const PromptGeom &g, int s, int &lo) {
 // Number `k` of the prompts' tiles, of which a prompt of n tokens has tiles_of(n): prompt by prompt, so that workgroups that run at the same time
 // read the same keys from their L2, the longest first, and of a prompt the deepest first (a tile's keys are all tokens up to its last
 // row), so that the last workgroups to start are short ones (the deepest of all prompts first: 24 prompts of up to 1500 tokens, 8 x 4 heads, 1.07 us
-// for the products of 32 keys and 256 rows instead of 0.85).  More than 64 prompts are taken in their own order.
+// for the products of 32 keys and 256 rows instead of 0.85).  More than 64 prompts are taken in their own order, 256 to a look (1000
+// prompts of 64 tokens, 8 heads of 128 over 2, 108 us, with 64 to a look 148).
 // `lo`, `n`: its prompt, `t`: its number there.  All lanes of a wave call it and get the same.
 template <class TilesOf>
 __device__ __forceinline__ bool tile_of(const PromptGeom &g, int k, int lane, int &lo, int &n, int &t, TilesOf tiles_of) {
@@ -37,11 +38,13 @@ __device__ __forceinline__ bool tile_of(const PromptGeom &g, int k, int lane, in
         t = __builtin_amdgcn_readlane(before + tiles, at) - 1 - k;
         return true;
     }
-    for (int base = 0; base < g.sequences; base += 64) {
-        int begin = 0, len = 0;
-        if (base + lane < g.sequences) len = prompt_of(g, base + lane, begin);
-        const int tiles = tiles_of(len);
-        int sum = tiles;  // over the lanes up to this one
+    for (int base = 0; base < g.sequences; base += 256) {  // four consecutive ones to a lane
+        int begin[5], tiles[4], own = 0;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) begin[i] = min(max(g.first[min(base + 4 * lane + i, g.sequences)], 0), g.tokens);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tiles[i] = tiles_of(max(0, begin[i + 1] - begin[i])), own += tiles[i];
+        int sum = own;  // over the lanes up to this one
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) {
             const int x = __shfl_up(sum, s);
@@ -50,12 +53,20 @@ __device__ __forceinline__ bool tile_of(const PromptGeom &g, int k, int lane, in
         const uint64_t beyond = __builtin_amdgcn_ballot_w64(sum > k);
         if (beyond) {
             const int at = __builtin_ctzll(beyond);
-            t = __shfl(tiles, at) - 1 - (k - __shfl(sum - tiles, at));
-            lo = __shfl(begin, at);
-            n = __shfl(len, at);
-            return true;
+            k -= __builtin_amdgcn_readlane(sum - own, at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int here = __builtin_amdgcn_readlane(tiles[i], at);
+                if (k < here) {
+                    lo = __builtin_amdgcn_readlane(begin[i], at);
+                    n = __builtin_amdgcn_readlane(begin[i + 1], at) - lo;
+                    t = here - 1 - k;
+                    return true;
+                }
+                k -= here;
+            }
         }
-        k -= __shfl(sum, 63);
+        k -= __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }

@@ -41,7 +41,7 @@ def test_grouped_heads(dtype):
 
 @pytest.mark.parametrize("count", [63, 64, 65, 255, 256, 257, 700])
 def test_many_prompts(count):
-    """Up to 64 prompts are taken by their length, more in their order, 64 to a look."""
+    """Up to 64 prompts are taken by their length, more in their order, 256 to a look."""
     g = torch.Generator().manual_seed(count)
     lens = torch.randint(0, 40, (count,), generator=g).tolist()
     lens[count // 2] = 300
