@@ -2,8 +2,8 @@
 //
 // A wave takes 32 rows of a query head; the four waves, heads of a group first, see nearly the same keys, whose rows and values' rows come to LDS once for
 // all of them, 32 keys to a stage, straight from global memory.  Two workgroups share a CU, so that one multiplies while the other one starts, waits or
-// writes its outputs, for which a tile of 256 rows (prompt_wide.hip) holds a CU for 10 us: 16 prompts of 200 tokens, 32 heads of 128 over 8, 24.7 us instead
-// of 32, of 500 66 instead of 78, one of 1024 29 instead of 35.  A wave reads every key and value from LDS for 32 rows only, twice as much per product,
+// writes its outputs, for which a tile of 256 rows (prompt_wide.hip) holds a CU for 10 us: 16 prompts of 200 tokens, 32 heads of 128 over 8, 24.5 us instead
+// of 32, of 500 69 instead of 78, one of 1024 27 instead of 35.  A wave reads every key and value from LDS for 32 rows only, twice as much per product,
 // which bounds it beyond that: one prompt of 16384 2085 us instead of 1890 (matrix cores 49 % busy; a third workgroup per CU, with three stages and no
 // products ahead, 2331; stages of 64 keys 2223; keys and values in registers a phase ahead, as in wide_tile.h, 2081).
 #include <type_traits>
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256, 2) void prompt_mid_kernel(PromptGeom g) {
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
     }
     const int limit = min(row0 + col, it.n - 1), limit_min = uniform(min(row0, it.n - 1));
-    f32x16 O[CB], acc;
+    f32x16 O[CB];
     float m, s;
     no_rows_yet(O, m, s);
     auto largest = [&](const f32x16 &x) {  // of a row's logits in a block, scaled
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void prompt_mid_kernel(PromptGeom g) {
         return x;
     };
     // Logits of block b that a row does not see become -inf; the reference is the largest logit of a row's first keys (wide_tile.h).
-    auto finish = [&](int b) {
+    auto finish = [&](f32x16 &acc, int b) {
         if (b * A::KEYS + A::KEYS - 1 > limit_min) {
             const int room = limit - b * A::KEYS - 4 * hf;
 #pragma unroll
@@ -127,53 +127,60 @@ __global__ __launch_bounds__(256, 2) void prompt_mid_kernel(PromptGeom g) {
     barrier(OneStage{});  // stage 0 is here, the query rows have been read
     request(2);
     int st = 0;
-    if (blocks > 0) {
-        acc = products(0);
-        finish(0);
-        for (; st < blocks; ++st) {
-            barrier(OneStage{});  // stage st + 1 is here, stage st - 1 done with
-            request(st + 3);
-            const f32x16 next = products(st + 1);  // beside this block's exponentials
-            const float mref = m == -INFINITY ? 0.f : m;
-            float sum[2] = {0.f, 0.f}, corr = 1.f;
-            bf16x8 pf[2];
+    // Block st, whose logits are `acc`; those of the next one become `next`.  (Two blocks to a round of the loop: with
+    // one, the logits are copied in each, and 16 prompts of 500 tokens take 71 us instead of 69.)
+    auto step = [&](f32x16 &acc, f32x16 &next) {
+        barrier(OneStage{});  // stage st + 1 is here, stage st - 1 done with
+        request(st + 3);
+        next = products(st + 1);  // beside this block's exponentials
+        const float mref = m == -INFINITY ? 0.f : m;
+        float sum[2] = {0.f, 0.f}, corr = 1.f;
+        bf16x8 pf[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float pr = fast_exp2(fmaf(acc[e], g.c_out, -mref));
+            sum[e & 1] += pr;
+            pf[e >> 3][e & 7] = (__bf16)pr;
+        }
+        const float all = sum[0] + sum[1];
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(all > kWideMost) != 0, 0)) {
+            // far above the reference: a new one, the largest logit, and these weights again
+            m = fmaxf(m, largest(acc));
+            const float mn = m == -INFINITY ? 0.f : m;
+            corr = fast_exp2(mref - mn);
+            s *= corr;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float pr = fast_exp2(fmaf(acc[e], g.c_out, -mref));
-                sum[e & 1] += pr;
+                const float pr = fast_exp2(fmaf(acc[e], g.c_out, -mn));
+                s += pr;
                 pf[e >> 3][e & 7] = (__bf16)pr;
             }
-            const float all = sum[0] + sum[1];
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(all > kWideMost) != 0, 0)) {
-                // far above the reference: a new one, the largest logit, and these weights again
-                m = fmaxf(m, largest(acc));
-                const float mn = m == -INFINITY ? 0.f : m;
-                corr = fast_exp2(mref - mn);
-                s *= corr;
+        } else {
+            s += all;
+        }
+        // (within that branch the compiler copies all outputs to other registers and back in every block: a prompt of 16384 2283 us)
+        if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float pr = fast_exp2(fmaf(acc[e], g.c_out, -mn));
-                    s += pr;
-                    pf[e >> 3][e & 7] = (__bf16)pr;
-                }
-            } else {
-                s += all;
-            }
-            // (within that branch the compiler copies all outputs to other registers and back in every block: a prompt of 16384 2283 us)
-            if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {
+            for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
+                for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
+        }
+        const __bf16 *sV = (const __bf16 *)(smem + A::off_values + st % S * A::vbytes);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
-            }
-            const __bf16 *sV = (const __bf16 *)(smem + A::off_values + st % S * A::vbytes);
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
-                    O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_fragment<D>(sV, 0, ks, cb, lane), pf[ks], O[cb], 0, 0, 0);
-            acc = next;
-            if (st + 1 < blocks) finish(st + 1);
+            for (int cb = 0; cb < CB; ++cb)
+                O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_fragment<D>(sV, 0, ks, cb, lane), pf[ks], O[cb], 0, 0, 0);
+        if (++st < blocks) finish(next, st);
+    };
+    if (blocks > 0) {
+        f32x16 x = products(0), y;
+        finish(x, 0);
+        while (true) {
+            step(x, y);
+            if (st >= blocks) break;
+            step(y, x);
+            if (st >= blocks) break;
         }
     }
     for (; st < stages; ++st) {  // (only its share of the loads)
