@@ -35,13 +35,14 @@ struct Rank {
 };
 __device__ __forceinline__ uint64_t rank_what(uint32_t key, int pos) { return (uint64_t)key << 32 | (uint32_t)~((uint32_t)pos ^ 0x80000000u); }
 
-constexpr int kEvictCandidates = 1024;
 template <int WAVES>
 struct EvictLds {
-    static constexpr int kBins = WAVES * 256;  // four to a thread
+    // four bins to a thread; tokens that are ranked by comparing them all, where last_to_go() takes longer (rows of 900, 4000, 32000 tokens: 300 alike
+    // 28, 32, 43 us ranked, 22, 32, 68 by it; 180 18, 26, 36)
+    static constexpr int kBins = WAVES * 256, kCandidates = 160 + 28 * WAVES;
     union {
         alignas(16) int hist[kBins];
-        Rank candidates[kEvictCandidates];
+        Rank candidates[kCandidates];
     };
     uint32_t all_low, all_above, from, to;
     int all_free;
@@ -63,42 +64,6 @@ __device__ __forceinline__ int wave_prefix(int x, int lane) {
     return x;
 }
 
-// The value of rank `rank` (from 0) in ascending order of value(j), j of [0, n) with in(j), digit by digit; `rank` becomes the rank among
-// those of this value.
-template <int WAVES, class In, class Value>
-__device__ __forceinline__ uint32_t value_of_rank(int n, int &rank, EvictLds<WAVES> &sm, In in, Value value) {
-    const int tid = threadIdx.x;
-    uint32_t found = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        if (tid < 256) sm.hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += WAVES * 64)
-            if (in(j)) {
-                const uint32_t x = value(j);
-                if (shift == 24 || (x >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&sm.hist[(x >> shift) & 255], 1);
-            }
-        __syncthreads();
-        if (tid < 64) {  // four digits per lane
-            int c[4], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] = sm.hist[tid * 4 + i], sum += c[i];
-            int below = wave_prefix(sum, tid) - sum;
-            if (rank >= below && rank < below + sum) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (rank >= below && rank < below + c[i]) sm.digit = tid * 4 + i, sm.rank = rank - below;
-                    below += c[i];
-                }
-            }
-        }
-        __syncthreads();
-        found |= (uint32_t)sm.digit << shift;
-        rank = sm.rank;
-    }
-    return found;
-}
-
 // What a workgroup reads of its tokens.
 struct EvictRows {
     const float *scores;
@@ -109,17 +74,6 @@ struct EvictRows {
     __device__ __forceinline__ uint32_t key_of(float score, int p) const { return going_key(score, safe(p)); }
     __device__ __forceinline__ uint32_t key_at(int j) const { return key_of(scores[j], pos_of(j)); }
 };
-
-// The last of `go` tokens to go, whatever their scores: key, position and place digit by digit, up to twelve sweeps.
-template <int WAVES>
-__device__ __forceinline__ Rank last_to_go_by_digits(const EvictRows &rows, int len, int go, EvictLds<WAVES> &sm) {
-    auto high_first = [&](int j) { return (uint32_t)rank_what(0, rows.pos_of(j)); };
-    int rank = go - 1;
-    const uint32_t T = value_of_rank(len, rank, sm, [](int) { return true; }, [&](int j) { return rows.key_at(j); });
-    const uint32_t P = value_of_rank(len, rank, sm, [&](int j) { return rows.key_at(j) == T; }, high_first);
-    const uint32_t J = value_of_rank(len, rank, sm, [&](int j) { return rows.key_at(j) == T && high_first(j) == P; }, [](int j) { return ~(uint32_t)j; });
-    return Rank{(uint64_t)T << 32 | P, J};
-}
 
 // Keys and values of moves, in rows of 16-byte chunks.
 __device__ __forceinline__ void move_rows(const EvictGeom &g, const int32_t *table, int h, const int2 *moves, int count, int tid, int threads) {
@@ -185,14 +139,14 @@ struct Eviction {
     }
 };
 
-// One histogram of the keys that may go, linear over their range: the bin of the last one to go, whose keys are then ranked against each other.
+// A histogram, linear over a range of keys: the bin of the last one to go, whose keys are then ranked against each other.
 template <int WAVES>
 struct EvictBins {
-    uint32_t low, slope;
+    uint32_t low, high, slope;
     // a little less than kBins 2^32 / (range + 1), which 64-bit division would take all waves 1.5 us for; 0: a bin for every key
-    __device__ __forceinline__ EvictBins(uint32_t low_, uint32_t above) : low(low_) {
+    __device__ __forceinline__ EvictBins(uint32_t low_, uint32_t high_) : low(low_), high(high_) {
         constexpr int kBins = EvictLds<WAVES>::kBins;
-        const uint32_t range = above - 1 - low;
+        const uint32_t range = high - low;
         slope = range < kBins ? 0u : (uint32_t)(kBins * 0x1p32f * (1.f - 0x1p-20f) * __builtin_amdgcn_rcpf((float)range + 1.f));
     }
     __device__ __forceinline__ int bin_of(uint32_t k) const { return (int)(slope ? __umulhi(k - low, slope) : k - low); }
@@ -218,7 +172,7 @@ struct EvictBins {
                 below += c[i];
             }
             sm.from = (uint32_t)first_of(sm.digit);
-            sm.to = (uint32_t)min(first_of(sm.digit + 1) - 1, (uint64_t)(kSafe - 1));
+            sm.to = (uint32_t)min(first_of(sm.digit + 1) - 1, (uint64_t)high);
         }
         __syncthreads();
     }
@@ -232,6 +186,7 @@ __device__ __forceinline__ void rank_candidates(EvictLds<WAVES> &sm, int keep, i
     for (int i = tid; i < in_bin; i += WAVES * 64) {
         const Rank r = sm.candidates[i];
         int smaller = 0;
+#pragma unroll 8
         for (int o = 0; o < in_bin; ++o) smaller += sm.candidates[o] < r;
         if (smaller == want) sm.last = r;
         // (what the rank says, too: the first want + 1 of them go)
@@ -240,6 +195,72 @@ __device__ __forceinline__ void rank_candidates(EvictLds<WAVES> &sm, int keep, i
         if (smaller > want && j >= keep) atomicAdd(&sm.movers[w], 1);
     }
     __syncthreads();
+}
+
+// The last one to go of many alike: number `want` of the `left` tokens whose keys lie in [k0, k1].  Histograms of these keys, then of the positions of an only
+// key, then of the places of an only position, until so few are left that they are ranked (63 rows of 1891 scores of 0 18 us, different scores 16; digit by
+// digit of key, position and place 36).
+template <int WAVES>
+__device__ __forceinline__ Rank last_to_go(const EvictRows &rows, int len, int want, int left, uint32_t k0, uint32_t k1, EvictLds<WAVES> &sm, int tid) {
+    constexpr int THREADS = WAVES * 64, U = 8;
+    uint32_t p0 = 0, p1 = ~0u, j0 = ~(uint32_t)(len - 1), j1 = ~0u;  // what is known of its position and place
+    // work(key, position's rank, place's rank) for the tokens left
+    auto sweep = [&](auto work) {
+        for (int first = tid; first < len; first += U * THREADS) {
+            float score[U];
+            int pos[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) score[u] = rows.scores[min(first + u * THREADS, len - 1)], pos[u] = rows.pos_of(min(first + u * THREADS, len - 1));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint64_t what = rank_what(rows.key_of(score[u], pos[u]), pos[u]);
+                const uint32_t k = (uint32_t)(what >> 32), p = (uint32_t)what, place = ~(uint32_t)(first + u * THREADS);
+                if (first + u * THREADS < len && k >= k0 && k <= k1 && p >= p0 && p <= p1 && place >= j0 && place <= j1) work(k, p, place);
+            }
+        }
+    };
+    auto narrow = [&](uint32_t &from, uint32_t &to, auto value) {
+        const EvictBins<WAVES> bins(from, to);
+        __syncthreads();
+        *(u32x4 *)&sm.hist[4 * tid] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        sweep([&](uint32_t k, uint32_t p, uint32_t place) { atomicAdd(&sm.hist[bins.bin_of(value(k, p, place))], 1); });
+        bins.find(sm, want + 1, tid);
+        from = sm.from;
+        to = sm.to;
+        want = sm.rank;
+        left = sm.in_bin;
+    };
+    while (left > sm.kCandidates && k0 < k1) narrow(k0, k1, [](uint32_t k, uint32_t, uint32_t) { return k; });
+    if (left > sm.kCandidates) {  // the range of their positions
+        uint32_t low = ~0u, high = 0;
+        sweep([&](uint32_t, uint32_t p, uint32_t) { low = min(low, p), high = max(high, p); });
+        low = reduce_lanes<1, 64>(low, OpMinU{});
+        high = reduce_lanes<1, 64>(high, OpMaxU{});
+        __syncthreads();
+        if (tid == 0) sm.all_low = ~0u, sm.all_above = 0;
+        __syncthreads();
+        if ((tid & 63) == 0) atomicMin(&sm.all_low, low), atomicMax(&sm.all_above, high);
+        __syncthreads();
+        p0 = sm.all_low;
+        p1 = sm.all_above;
+    }
+    while (left > sm.kCandidates && p0 < p1) narrow(p0, p1, [](uint32_t, uint32_t p, uint32_t) { return p; });
+    while (left > sm.kCandidates) narrow(j0, j1, [](uint32_t, uint32_t, uint32_t place) { return place; });
+    __syncthreads();
+    if (tid == 0) sm.n_candidates = 0;
+    __syncthreads();
+    sweep([&](uint32_t k, uint32_t p, uint32_t place) { sm.candidates[atomicAdd(&sm.n_candidates, 1)] = Rank{(uint64_t)k << 32 | p, place}; });
+    __syncthreads();
+    for (int i = tid; i < left; i += THREADS) {
+        const Rank r = sm.candidates[i];
+        int smaller = 0;
+#pragma unroll 8
+        for (int o = 0; o < left; ++o) smaller += sm.candidates[o] < r;
+        if (smaller == want) sm.last = r;
+    }
+    __syncthreads();
+    return sm.last;
 }
 
 // The tokens' keys in LDS, `steps` steps of 64 tokens of a wave, one lane each, which alone reads them.  Returns the number of moves.
@@ -325,7 +346,8 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     if (go > 1)
         *(u32x4 *)&sm.hist[4 * tid] = u32x4{0, 0, 0, 0};
     of_all();
-    if (go > free_keys) {  // all that may go do, and protected ones by their position: other keys of the same order, positions in turns
+    const bool turned = go > free_keys;
+    if (turned) {  // all that may go do, and protected ones by their position: other keys of the same order, positions in turns
         __syncthreads();
         if (tid == 0) sm.all_low = kSafe, sm.all_above = 0, sm.all_free = 0;
         for (int t = 0; t < steps; ++t)
@@ -369,7 +391,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
     int gaps = 0, movers = 0;
     bool found = false;
     {
-        const EvictBins<WAVES> bins(low, above);
+        const EvictBins<WAVES> bins(low, above - 1);
 #pragma unroll 4
         for (int t = 0; t < steps; ++t) {
             const uint32_t k = key[t * 64];
@@ -377,7 +399,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
         }
         bins.find(sm, go, tid);
         const uint32_t from = sm.from, to = sm.to;
-        if (sm.in_bin <= kEvictCandidates) {
+        if (sm.in_bin <= sm.kCandidates) {
             found = true;
             auto note = [&](int t) {
                 const uint32_t k = key[t * 64];
@@ -414,7 +436,7 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
             if ((uint32_t)(r.what >> 32) == last_key && last < r) keys[~r.place] = kSafe;
         }
     } else {
-        last = last_to_go_by_digits(rows, len, go, sm);
+        last = turned ? last_to_go(rows, len, go - 1, len, 0u, ~0u, sm, tid) : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
         last_key = 0;
         for (int t = 0; t < steps; ++t)
             if (base + t * 64 < len) key[t * 64] = last < rank_of(t, rows.key_at(base + t * 64)) ? kSafe : 0u;
@@ -492,13 +514,13 @@ __device__ __forceinline__ int evict_from_memory(Eviction &e, EvictLds<WAVES> &s
     int gaps = 0, movers = 0;
     bool found = false;
     if (go <= sm.all_free) {
-        const EvictBins<WAVES> bins(sm.all_low, sm.all_above);
+        const EvictBins<WAVES> bins(sm.all_low, sm.all_above - 1);
         sweep([&](int, uint32_t k, int) {
             if (k != kSafe) atomicAdd(&sm.hist[bins.bin_of(k)], 1);
         });
         bins.find(sm, go, tid);
         const uint32_t from = sm.from, to = sm.to;
-        if (sm.in_bin <= kEvictCandidates) {
+        if (sm.in_bin <= sm.kCandidates) {
             found = true;
             sweep([&](int j, uint32_t k, int p) {
                 if (k >= from && k <= to) sm.candidates[atomicAdd(&sm.n_candidates, 1)] = Rank{rank_what(k, p), ~(uint32_t)j};
@@ -511,8 +533,8 @@ __device__ __forceinline__ int evict_from_memory(Eviction &e, EvictLds<WAVES> &s
         }
     }
     auto goes = [&](int j, uint32_t k, int p) { return !(last < Rank{rank_what(k, p), ~(uint32_t)j}); };
-    if (!found) {  // more protected tokens go, or too many keys are alike
-        last = last_to_go_by_digits(rows, len, go, sm);
+    if (!found) {  // protected tokens go, or too many keys are alike
+        last = go > sm.all_free ? last_to_go(rows, len, go - 1, len, 0u, ~0u, sm, tid) : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
         sweep([&](int j, uint32_t k, int p) {
             const bool out = goes(j, k, p);
             gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(out && j < min(keep, end)));

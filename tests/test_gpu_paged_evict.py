@@ -127,6 +127,20 @@ def test_long_sequences_of_any_kind(in_place):
     Evictions(23, [n, 36000], kv_heads=1, d=64, budget=900, page=64, holes={(1, 300): -1}, in_place=in_place).check()
 
 
+@pytest.mark.parametrize("n", [900, 3000, 9000, 40000])
+def test_many_alike(n):
+    """More of one score than are compared with each other; of one position too; more protected tokens than the budget."""
+    rng = np.random.default_rng(n)
+    shape = (1, 2, n)
+    few = torch.from_numpy(rng.integers(0, 3, shape).astype(np.float32))
+    some = torch.from_numpy(np.where(rng.random(shape) < 0.4, 0.5, rng.random(shape)).astype(np.float32))
+    at = torch.from_numpy(rng.integers(0, n, shape).astype(np.int32))
+    for scores, pos, budget in ((few, at, n // 2), (some, at, n // 3), (torch.zeros(shape), at, n - 500), (torch.zeros(shape), at // 100, 700),
+                                (torch.zeros(shape), torch.zeros(shape, dtype=torch.int32), n // 2), (few, at % 2, n - 1)):
+        Evictions(24, [n], kv_heads=2, d=64, budget=budget, scores=scores, pos=pos, page=64, slots=n, seen=[10 ** 6]).check()
+    Evictions(25, [n], kv_heads=2, d=64, budget=n // 2, recent=n // 2, scores=some, pos=at % 5, page=64, slots=n, seen=[3]).check()
+
+
 def test_shared_scores():
     """One row of scores for all heads, expanded, into outputs of their own."""
     base = torch.rand(2, 1, 160, generator=torch.Generator().manual_seed(1))
