@@ -302,6 +302,7 @@ struct PromptGeom {
 struct PromptPlan {
     int rows;       // of a tile: 16 (fp32), 32, 128 (prompt_mid.hip) or 256 (prompt_wide.hip)
     int64_t items;  // workgroups, at most (the prompts' lengths are known on the device)
+    bool staged;    // bf16, d = 64, tiles of 32 rows: keys by way of LDS (narrow_tile.h), as with d = 128
 };
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st);
 // prompt_wide.hip

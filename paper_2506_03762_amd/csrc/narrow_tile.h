@@ -30,6 +30,45 @@ __device__ __forceinline__ void no_rows_yet(f32x16 (&O)[CB], float &m, float &s)
 #pragma unroll
         for (int v = 0; v < 16; ++v) O[cb][v] = 0.f;
 }
+// The weights of the 32 keys from kb on, by their products `acc`: rounded to bf16 in `pf`, added to s; reference and outputs moved where these exceed it.
+template <int CB, class Block>
+__device__ __forceinline__ void weigh_block(f32x16 &acc, int kb, uint32_t there, int limit, int limit_min, float c_out, int hf, float &m, float &s,
+                                            f32x16 (&O)[CB], bf16x8 (&pf)[2], Block block) {
+    if (there != 0xffffffffu || kb + 31 > limit_min) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int at = 8 * (v >> 2) + 4 * hf + (v & 3);
+            if (kb + at > limit || !((there >> at) & 1)) acc[v] = -INFINITY;
+        }
+    }
+    block(kb, acc);
+    float amax = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) amax = fmaxf(amax, acc[v]);
+    amax = combine_lane_xor<32>(amax, OpMax{});
+    // (the reference follows the running maximum lazily: it moves when a block's exceeds it by more than kRefSlack)
+    const float bm = amax * c_out;
+    const float mn = bm > m + kRefSlack ? bm : m;
+    const float mref = mn == -INFINITY ? 0.f : mn;
+    const float corr = fast_exp2(m - mref);
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float pr = fast_exp2(fmaf(acc[8 * ks + e], c_out, -mref));
+            sum[e & 1] += pr;
+            pf[ks][e] = (__bf16)pr;
+        }
+    s = s * corr + (sum[0] + sum[1]);
+    m = mn;
+    if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
+    }
+}
 // ONCE: the values are read past the caches, as no other tile reads them (64 caches of up to 4096 tokens, 8 x 4 heads of 128 channels 160 us, so 156; the
 // keys too 191: a lane's pieces of a row come with eight loads, which then read it again).  `limit`: the last key that the lane's row sees.
 // `block(kb, acc)` is told the products of the 32 keys from kb on, those that a row does not see -inf.
@@ -88,47 +127,77 @@ __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf
         __builtin_amdgcn_sched_barrier(0);
         load_keys(here.k);
         __builtin_amdgcn_sched_barrier(0);
-        if (there != 0xffffffffu || kb + 31 > limit_min) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int at = 8 * (v >> 2) + 4 * hf + (v & 3);
-                if (kb + at > limit || !((there >> at) & 1)) acc[v] = -INFINITY;
-            }
-        }
-        block(kb, acc);
-        float amax = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) amax = fmaxf(amax, acc[v]);
-        amax = combine_lane_xor<32>(amax, OpMax{});
-        // (the reference follows the running maximum lazily: it moves when a block's exceeds it by more than kRefSlack)
-        const float bm = amax * c_out;
-        const float mn = bm > m + kRefSlack ? bm : m;
-        const float mref = mn == -INFINITY ? 0.f : mn;
-        const float corr = fast_exp2(m - mref);
-        float sum[2] = {0.f, 0.f};
         bf16x8 pf[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float pr = fast_exp2(fmaf(acc[8 * ks + e], c_out, -mref));
-                sum[e & 1] += pr;
-                pf[ks][e] = (__bf16)pr;
-            }
-        s = s * corr + (sum[0] + sum[1]);
-        m = mn;
-        if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) O[cb][v] *= corr;
-        }
+        weigh_block(acc, kb, there, limit, limit_min, c_out, hf, m, s, O, pf, block);
         const __bf16 *sV = (const __bf16 *)(smem + (wave * 2 + buf) * A::v_bytes);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_fragment<D>(sV, 0, ks, cb, lane), pf[ks], O[cb], 0, 0, 0);
+    }
+    wait_loads<0>();
+}
+
+// The same with the keys by way of LDS, too: whole rows, of which a lane's pieces straight from memory are a quarter of a line each, eight times.  Keys and values are
+// read from there together, then the next block's are requested: a longer chain than above, but less for the L1, which all waves of a CU share.  d = 128, one
+// prompt of 512 tokens, 32 heads over 8 15.9 us, so 13.6, of 2048, 8 over 2, 36.5, 29.9, of 4096, 2 heads 42.3, 40.5; d = 64, 9 of up to 777, 6 heads over 2, 13.5,
+// 11.7, one of 4096, 2 heads, a workgroup per CU, 25.0, 28.3.  Caches in pages, whose rows' addresses come lane by lane: 64 of 1000 tokens 46, 53.
+template <int D>
+struct StagedRows {
+    static constexpr int k_bytes = KeyRows<D>::bytes(32), bytes = k_bytes + 32 * D * 2;
+    static constexpr size_t stage_bytes = 4 * bytes;
+};
+template <int D, class Keys>
+__device__ __forceinline__ void staged_sweep(const Keys &keys, const bf16x8 (&qf)[D / 16], int limit, float c_out, char *smem, int lane, int wave,
+                                             f32x16 (&O)[D / 32], float &m, float &s) {
+    using A = NarrowRows<D>;
+    using S = StagedRows<D>;
+    using R = KeyRows<D>;
+    constexpr int KS = D / 16, CB = D / 32;
+    const int hf = lane >> 5, limit_min = -reduce_lanes<1, 32>(-limit, OpMaxI{});
+    char *own = smem + wave * S::bytes;
+    const uint32_t lds0 = uniform((int)((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)own));
+    const int lr = lane / A::CPR, kchunk = (lane % A::CPR) ^ R::swizzle(lr), vchunk = (lane % A::CPR) ^ value_chunk_swizzle<D>(lr);
+    auto load_to_lds = [&](const __bf16 *from, int to) {
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds0 + to) : "memory");
+    };
+    auto request = [&](int kb) {
+#pragma unroll
+        for (int j = 0; j < A::NI; ++j) load_to_lds(keys.at(kb + j * A::RPI + lr, 0).k + kchunk * 8, j * R::group);
+#pragma unroll
+        for (int j = 0; j < A::NI; ++j) load_to_lds(keys.at(kb + j * A::RPI + lr, 0).v + vchunk * 8, S::k_bytes + j * 1024);
+    };
+    int kb = keys.begin + wave * 32;
+    request(kb);
+    const int place = key_place<D>(lane);
+    const __bf16 *sV = (const __bf16 *)(own + S::k_bytes);
+    for (; kb < keys.end; kb += A::STEP) {
+        __builtin_amdgcn_sched_barrier(0);
+        wait_loads<0>();
+        asm volatile("" ::: "memory");
+        bf16x8 a[KS], vf[2 * CB];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) a[ks] = key_fragment(own, place, ks);
+#pragma unroll
+        for (int i = 0; i < 2 * CB; ++i) vf[i] = value_fragment<D>(sV, 0, i / CB, i % CB, lane);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(a[ks]));
+#pragma unroll
+        for (int i = 0; i < 2 * CB; ++i) asm volatile("" : "+v"(vf[i]));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        request(kb + A::STEP);
+        f32x16 acc;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], qf[ks], acc, 0, 0, 0);
+        bf16x8 pf[2];
+        const int left = keys.end - kb;
+        weigh_block(acc, kb, left >= 32 ? 0xffffffffu : (1u << left) - 1, limit, limit_min, c_out, hf, m, s, O, pf, [](int, const f32x16 &) {});
+#pragma unroll
+        for (int i = 0; i < 2 * CB; ++i) O[i % CB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[i / CB], O[i % CB], 0, 0, 0);
     }
     wait_loads<0>();
 }
@@ -288,9 +357,9 @@ __device__ __forceinline__ void meet_waves(int rows, bool live_row, f32x16 (&O)[
 }
 
 // LDS of a kernel of these sweeps: the values' blocks (fp32: the query rows), later the waves' results.
-template <class T, int D>
+template <class T, int D, bool STAGED = false>
 constexpr size_t narrow_lds() {
-    const size_t swept = sizeof(T) == 2 ? NarrowRows<D>::stage_bytes : (size_t)32 * f32_ld(D) * 4;
+    const size_t swept = sizeof(T) == 4 ? (size_t)32 * f32_ld(D) * 4 : STAGED ? StagedRows<D>::stage_bytes : NarrowRows<D>::stage_bytes;
     return swept > WaveMerge<D>::bytes ? swept : WaveMerge<D>::bytes;
 }
 // Its workgroups per CU, at least.  Three where their LDS (32 KB each) and registers allow it without spills, bf16 with d = 64: there latency is what a

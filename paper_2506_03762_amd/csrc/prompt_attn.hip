@@ -6,9 +6,9 @@
 // joined and a call is one launch.  Tiles have 32 rows (here; narrow_tile.h), fp32 also 16 (small_tile.h), 128 (prompt_mid.hip) or 256 (prompt_wide.hip);
 // plan_prompt() chooses.
 //
-// Here four waves divide the keys of 32 rows of one head: the shortest chain for few rows, bound by the latency of its blocks of 128 keys (d = 64 0.9 us, of
-// which the loads are requested one block ahead; 128 1.65 us), but every tile reads its keys and values from the L2 again.  9 prompts of up to 777 tokens, 6 heads of
-// 64 over 2: 12.6 us.  fp32: one prompt of 512, 2 heads of 64, 9.9 us in 64 tiles of 16 rows, 15.2 in 32 of 32, each bound by the products of its rows; of
+// Here four waves divide the keys of 32 rows of one head: the shortest chain for few rows, bound by the latency of its blocks of 128 keys (d = 64 0.7 us, 128
+// 1.4 us, loads requested one block ahead) and the L1, but every tile reads its keys and values from the L2 again.  9 prompts of up to 777 tokens, 6 heads of 64
+// over 2: 10.8 us.  fp32: one prompt of 512, 2 heads of 64, 9.9 us in 64 tiles of 16 rows, 15.2 in 32 of 32, each bound by the products of its rows; of
 // 4096, 32 heads of 128 over 8, 1276 us, 108 TFLOP/s, 0.70 of a library's product of 8192^3.  With eight waves to a tile every shape was slower.
 #include <limits.h>
 
@@ -18,10 +18,10 @@
 
 namespace aha {
 
-template <class T, int D, int ROWS>
+template <class T, int D, int ROWS, bool STAGED>
 __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_kernel(PromptGeom g) {
     using A = Tile<T, D, ROWS>;
-    __shared__ __attribute__((aligned(1024))) char smem[A::lds];
+    __shared__ __attribute__((aligned(1024))) char smem[STAGED ? narrow_lds<T, D, true>() : A::lds];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane % ROWS;
     PromptTile it;
     if (!prompt_tile(g, ROWS, (int)blockIdx.x, lane, it)) return;
@@ -39,7 +39,8 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
         bf16x8 qf[D / 16];
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + (lane >> 5) * 8 + ks * 16);
-        narrow_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s, [](int, const f32x16 &) {});
+        if constexpr (STAGED) staged_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s);
+        else narrow_sweep<D>(keys, qf, limit, g.c_out, smem, lane, wave, O, m, s, [](int, const f32x16 &) {});
     } else if constexpr (ROWS == 16) {
         f32x4 qf[D / 16];
 #pragma unroll
@@ -62,18 +63,21 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
         });
 }
 
-template <class T, int ROWS>
-static hipError_t launch_prompt_t(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
-    if (g.d == 64) hipLaunchKernelGGL((prompt_narrow_kernel<T, 64, ROWS>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((prompt_narrow_kernel<T, 128, ROWS>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
+template <class T, int D, int ROWS, bool STAGED>
+static hipError_t launch_narrow(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
+    hipLaunchKernelGGL((prompt_narrow_kernel<T, D, ROWS, STAGED>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
     return hipGetLastError();
 }
 
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
     if (pl.rows == 128) return launch_prompt_mid(g, pl, st);
     if (pl.rows > 32) return launch_prompt_wide(g, pl, st);
-    if (g.dtype == AHA_BF16) return launch_prompt_t<__bf16, 32>(g, pl, st);
-    return pl.rows == 16 ? launch_prompt_t<float, 16>(g, pl, st) : launch_prompt_t<float, 32>(g, pl, st);
+    if (g.dtype == AHA_BF16) {
+        if (g.d == 128) return launch_narrow<__bf16, 128, 32, true>(g, pl, st);
+        return pl.staged ? launch_narrow<__bf16, 64, 32, true>(g, pl, st) : launch_narrow<__bf16, 64, 32, false>(g, pl, st);
+    }
+    if (pl.rows == 16) return g.d == 64 ? launch_narrow<float, 64, 16, false>(g, pl, st) : launch_narrow<float, 128, 16, false>(g, pl, st);
+    return g.d == 64 ? launch_narrow<float, 64, 32, false>(g, pl, st) : launch_narrow<float, 128, 32, false>(g, pl, st);
 }
 
 }  // namespace aha

@@ -222,15 +222,15 @@ static PromptPlan plan_prompt(const aha_prompt *p) {
     PromptPlan pl{};
     // The cheapest tiles by an estimate for prompts of equal lengths (the host knows no others): the first ones' cost, all of a prompt's keys, and the average
     // one's for every further round.  The numbers are fitted to the times of 324 shapes (1 to 64 prompts of 20 to 8192 tokens, 2 to 64 heads): what they
-    // choose is 0.7 % slower than the fastest tiles on average, and 1.2 times at worst (16 prompts of 100 tokens, 8 heads over 2: 10.3, 8.6, 12.2 us in the order of
-    // the table).  d = 128, 32 heads over 8: one prompt of 512 14.8, 17.0, 21.7, 1024 36, 29.3, 34.9, 4096 310, 158, 138, 16 of 200 55, 24.7, 32;
-    // 8 over 2: one of 2048 36.6, 49.4, 59, 16 of 64 7.6, 7.1, 10.3.  d = 64, 16 heads: one of 1024 13.8, 21.8, 28.4, of 4096 94, 80, 88, 16 of
-    // 500 49, 29.3, 28.9.
+    // choose is 0.8 % (d = 64 0.1) slower than the fastest tiles on average, and 1.2 times at worst (one prompt of 8192, 6 heads over 2: 178, 173, 206 us in the
+    // order of the table).  d = 128, 32 heads over 8: one prompt of 512 13.5, 16.0, 21.9, 1024 31.1, 26.8, 34.8, 4096 241, 146, 135, 16 of 200 55, 23.5,
+    // 32; 8 over 2: one of 2048 29.2, 45, 58, 16 of 64 7.6, 6.8, 10.2.  d = 64, 16 heads: one of 1024 12.4, 20.4, 28.5, of 4096 71, 70, 88, 16 of 500
+    // 42.5, 27.1, 28.6.
     // fp32, 300 shapes: 1.0 and 0.6 % (1.15 and 1.4 times: 16 prompts of 20 tokens, 16 heads, 8.0, 10.9 in the order of the table).  d = 64: one prompt of 512, 2
     // heads, 10.7, 16.0, 8 heads of 2048 71, 69, of 4096 245, 191; d = 128: 2 heads of 1024 28.9, 43.9, 8 of 1024 56, 47.
     static constexpr PromptTiles kTiles[2][3] = {
-        {{32, 32, 512, 5.94f, .235f, 1.f}, {128, 32, 512, 5.38f, .49f, 1.26f}, {256, 64, 256, 5.81f, .55f, 1.f}},    // d = 64
-        {{32, 32, 512, 8.9f, .4125f, 1.f}, {128, 32, 512, 8.2f, .66f, 1.3f}, {256, 64, 256, 13.4f, .66f, 1.f}}};  // d = 128
+        {{32, 32, 512, 5.84f, .17f, 1.14f}, {128, 32, 512, 5.11f, .5f, 1.27f}, {256, 64, 256, 6.31f, .52f, 1.16f}},  // d = 64
+        {{32, 32, 512, 8.86f, .35f, 1.f}, {128, 32, 512, 7.73f, .6f, 1.14f}, {256, 64, 256, 15.34f, .57f, .92f}}};   // d = 128
     const int64_t prompts = std::min<int64_t>(p->sequences, p->tokens), group = p->n_q_heads / p->n_kv_heads, n = (p->tokens + prompts - 1) / prompts;
     static constexpr PromptTiles kTilesF32[2][2] = {{{16, 16, 256, 4.11f, .6f, .48f}, {32, 32, 256, 6.55f, .72f, .68f}},    // d = 64
                                                     {{16, 16, 256, 5.41f, 1.18f, .67f}, {32, 32, 256, 9.29f, 1.15f, .73f}}};  // d = 128
@@ -243,6 +243,7 @@ static PromptPlan plan_prompt(const aha_prompt *p) {
         if (time >= least) return;
         least = time;
         pl.rows = t.rows;
+        pl.staged = tiles > 256;  // (more than one workgroup to a CU: over 162 shapes 0.4 % slower than the faster one on average; never 6, always 0.9)
         // at most: one unit's rows, and one tile, of every prompt are not full
         pl.items = ((p->tokens + (t.unit - 1) * prompts) / t.unit * group + prompts * (heads - 1)) / heads * p->n_kv_heads;
         if (heads == 1) pl.items = (pl.items / group + 7) / 8 * 8 * group;

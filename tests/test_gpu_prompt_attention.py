@@ -48,6 +48,14 @@ def test_many_prompts(count):
     Prompts(9, lens, q_heads=2, kv_heads=1, d=64).check()
 
 
+@pytest.mark.parametrize("seed, lens, heads, kv_heads, more", [
+    (50, [700, 65, 333, 1, 500, 31, 260, 449], 6, 2, dict(layout="htd", gap=3)), (51, [700, 65, 333, 1, 500, 31, 260, 449], 4, 4, dict(pad=8)),
+    (52, [1300], 8, 2, dict(hot=5.0)), (53, [900, 800], 6, 2, dict(scale=1.5)), (54, [1500], 8, 4, dict(scale=0.0)), (55, [640, 641], 7, 1, {})])
+def test_more_tiles_of_32_rows_than_compute_units(seed, lens, heads, kv_heads, more):
+    """Their keys go by way of LDS."""
+    Prompts(seed, lens, q_heads=heads, kv_heads=kv_heads, d=64, **more).check()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_fp32_problems_that_fill_the_chip(d):
     """Few rows go to tiles of 16, these to tiles of 32."""
