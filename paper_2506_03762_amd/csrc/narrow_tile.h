@@ -139,8 +139,8 @@ __device__ __forceinline__ void narrow_sweep(const Keys &keys, const bf16x8 (&qf
     wait_loads<0>();
 }
 
-// The same with the keys by way of LDS, too: whole rows, of which a lane's pieces straight from memory are a quarter of a line each, eight times.  Keys and values are
-// read from there together, then the next block's are requested: a longer chain than above, but less for the L1, which all waves of a CU share.  d = 128, one
+// The same with the keys by way of LDS, too: whole rows, of which a lane's pieces straight from memory are a quarter of a line each, eight times.  Keys and
+// values are read from there together, then the next block's are requested: a longer chain than above, but less for the L1, which all waves of a CU share.  d = 128, one
 // prompt of 512 tokens, 32 heads over 8 15.9 us, so 13.6, of 2048, 8 over 2, 36.5, 29.9, of 4096, 2 heads 42.3, 40.5; d = 64, 9 of up to 777, 6 heads over 2, 13.5,
 // 11.7, one of 4096, 2 heads, a workgroup per CU, 25.0, 28.3.  Caches in pages, whose rows' addresses come lane by lane: 64 of 1000 tokens 46, 53.
 template <int D>

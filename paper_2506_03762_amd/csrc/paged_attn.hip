@@ -9,7 +9,8 @@
 //
 // Bound by memory: keys and values are read once, for all query heads of their KV head, and two operations per element and head are far below what the
 // matrix core gives.  64 caches of up to 4096 tokens, 8 heads of 128: 670 MB in 145 us, 4.6 TB/s (a copy reaches 4.95), joining 12 more; one cache
-// of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.5 + 4.5, of which 14 are the 67 MB.  Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
+// of 131072 tokens 540 MB in 113 us, 4.75 TB/s, joining 11; 8 caches of 2049 tokens 18.5 + 4.5, of which 14 are the 67 MB.
+// Small caches are a chain: 8 of 64 tokens 9 us, 5 of them the launch's.
 #include <limits.h>
 
 #include "small_tile.h"
@@ -270,9 +271,10 @@ template <class T, int D>
 static hipError_t launch_paged_t(const PagedGeom &g, const PagedPlan &pl, void *ws, hipStream_t st) {
     float *part_o = (float *)ws, *dots = g.slots > 0 ? (float *)((char *)ws + pl.off_dots) : nullptr;
     float2 *part_ms = (float2 *)((char *)ws + pl.off_ms), *part_ms2 = (float2 *)((char *)ws + pl.off_ms2);
-    hipError_t e;
-    if constexpr (sizeof(T) == 4) e = pl.rows == 16 ? launch_parts<T, D, 16>(g, pl, part_o, part_ms, part_ms2, dots, st) : launch_parts<T, D, 32>(g, pl, part_o, part_ms, part_ms2, dots, st);
-    else e = launch_parts<T, D, 32>(g, pl, part_o, part_ms, part_ms2, dots, st);
+    auto launch = launch_parts<T, D, 32>;
+    if constexpr (sizeof(T) == 4)
+        if (pl.rows == 16) launch = launch_parts<T, D, 16>;
+    const hipError_t e = launch(g, pl, part_o, part_ms, part_ms2, dots, st);
     if (e != hipSuccess || pl.one) return e;
     const int score_wgs = g.slots > 0 ? (int)((pl.ld + kJoinKeys - 1) / kJoinKeys) : 0;
     auto join = [&](auto kernel, int rows) {

@@ -1,8 +1,8 @@
 // One pass of a tile of 16 query rows over a range of keys, fp32: as in narrow_tile.h, on v_mfma_f32_16x16x4_f32.
 //
 // The matrix core's fp32 rate is the same and half of a tile of 32 rows is empty where there are up to 16: a block of 32 keys and 64 channels takes 2048 cycles
-// instead of 4096.  With more rows it reads the keys twice as often.  A lane's channels of a key row and a query row are 16 i + 4 (lane / 16) .. + 3, one of which is
-// a contraction step's for its quarter of the wave; its weights are those of its row, lane % 16, and the keys 16 t + 4 (lane / 16) + r, element r of
+// instead of 4096.  With more rows it reads the keys twice as often.  A lane's channels of a key row and a query row are 16 i + 4 (lane / 16) .. + 3, one of
+// which is a contraction step's for its quarter of the wave; its weights are those of its row, lane % 16, and the keys 16 t + 4 (lane / 16) + r, element r of
 // accumulator t, which the second product takes one element at a time, four keys to a step.
 #pragma once
 
