@@ -347,9 +347,11 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
         *(u32x4 *)&sm.hist[4 * tid] = u32x4{0, 0, 0, 0};
     of_all();
     const bool turned = go > free_keys;
+    const int unprotected = free_keys;
     if (turned) {  // all that may go do, and protected ones by their position: other keys of the same order, positions in turns
         __syncthreads();
         if (tid == 0) sm.all_low = kSafe, sm.all_above = 0, sm.all_free = 0;
+#pragma unroll 8
         for (int t = 0; t < steps; ++t)
             if (base + t * 64 < len)
                 key[t * 64] = key[t * 64] == kSafe ? min(max((uint32_t)rank_what(0, rows.pos_of(base + t * 64)), 1u), kSafe - 1) : 0u;
@@ -436,8 +438,10 @@ __device__ __forceinline__ int evict_in_lds(Eviction &e, EvictLds<WAVES> &sm, ui
             if ((uint32_t)(r.what >> 32) == last_key && last < r) keys[~r.place] = kSafe;
         }
     } else {
-        last = turned ? last_to_go(rows, len, go - 1, len, 0u, ~0u, sm, tid) : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
+        last = turned ? last_to_go(rows, len, go - 1 - unprotected, len - unprotected, kSafe, kSafe, sm, tid)
+                      : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
         last_key = 0;
+#pragma unroll 8
         for (int t = 0; t < steps; ++t)
             if (base + t * 64 < len) key[t * 64] = last < rank_of(t, rows.key_at(base + t * 64)) ? kSafe : 0u;
         for (int t = 0; t < front_steps; ++t) gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[t * 64] == 0 && base + t * 64 < keep));
@@ -534,7 +538,8 @@ __device__ __forceinline__ int evict_from_memory(Eviction &e, EvictLds<WAVES> &s
     }
     auto goes = [&](int j, uint32_t k, int p) { return !(last < Rank{rank_what(k, p), ~(uint32_t)j}); };
     if (!found) {  // protected tokens go, or too many keys are alike
-        last = go > sm.all_free ? last_to_go(rows, len, go - 1, len, 0u, ~0u, sm, tid) : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
+        last = go > sm.all_free ? last_to_go(rows, len, go - 1 - sm.all_free, len - sm.all_free, kSafe, kSafe, sm, tid)
+                                : last_to_go(rows, len, sm.rank, sm.in_bin, sm.from, sm.to, sm, tid);
         sweep([&](int j, uint32_t k, int p) {
             const bool out = goes(j, k, p);
             gaps += __builtin_popcountll(__builtin_amdgcn_ballot_w64(out && j < min(keep, end)));
