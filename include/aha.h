@@ -565,6 +565,9 @@ typedef struct aha_prompt {
 } aha_prompt;
 
 int32_t aha_prompt_attention_workspace_bytes(const aha_prompt *p, size_t *out_bytes);
+/* Rows of a tile that a call works in, which say what kernel runs: 16, 32, 128 or 256.  Results do not depend on it
+ * beyond their rounding; for tests and profiles. */
+int32_t aha_prompt_attention_tile_rows(const aha_prompt *p, int32_t *out_rows);
 int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, const void *v,
                              const int32_t *first, void *out, float *lse, void *workspace,
                              size_t workspace_bytes, void *stream);

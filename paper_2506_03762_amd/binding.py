@@ -36,7 +36,7 @@ EXPORTS = ("aha_workspace_bytes", "aha_prefill_scores", "aha_prefill_scores_lse"
            "aha_compact_kv", "aha_decode_step", "aha_decode_step_static", "aha_profile_events",
            "aha_exchange_looks", "aha_rotate", "aha_append_paged",
            "aha_shared_attention_workspace_bytes", "aha_shared_attention",
-           "aha_prompt_attention_workspace_bytes", "aha_prompt_attention",
+           "aha_prompt_attention_workspace_bytes", "aha_prompt_attention_tile_rows", "aha_prompt_attention",
            "aha_paged_attention_workspace_bytes", "aha_paged_attention",
            "aha_paged_evict_workspace_bytes", "aha_paged_evict", "aha_last_error",
            "aha_version")
@@ -131,6 +131,7 @@ def load() -> ctypes.CDLL:
     lib.aha_shared_attention.argtypes = [sp, gp] + [vp] * 13 + [sz, vp]
     mp, cp = ctypes.POINTER(aha_prompt), ctypes.POINTER(aha_paged)
     lib.aha_prompt_attention_workspace_bytes.argtypes = [mp, ctypes.POINTER(sz)]
+    lib.aha_prompt_attention_tile_rows.argtypes = [mp, ctypes.POINTER(i32)]
     lib.aha_prompt_attention.argtypes = [mp] + [vp] * 7 + [sz, vp]
     lib.aha_paged_attention_workspace_bytes.argtypes = [cp, gp, ctypes.POINTER(sz)]
     lib.aha_paged_attention.argtypes = [cp, gp] + [vp] * 11 + [sz, vp]
@@ -603,6 +604,13 @@ class PromptAttention(_Described):
 def prompt_attention_workspace_bytes(p: PromptAttention) -> int:
     out = ctypes.c_size_t(0)
     _check(load().aha_prompt_attention_workspace_bytes(p, ctypes.byref(out)))
+    return out.value
+
+
+def prompt_attention_tile_rows(p: PromptAttention) -> int:
+    """Rows of a tile that a call works in, which say what kernel runs (for tests and profiles)."""
+    out = ctypes.c_int32(0)
+    _check(load().aha_prompt_attention_tile_rows(p, ctypes.byref(out)))
     return out.value
 
 

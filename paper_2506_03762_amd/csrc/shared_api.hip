@@ -455,6 +455,14 @@ int32_t aha_prompt_attention_workspace_bytes(const aha_prompt *p, size_t *out_by
     return AHA_OK;
 }
 
+int32_t aha_prompt_attention_tile_rows(const aha_prompt *p, int32_t *out_rows) {
+    if (!out_rows) return fail(AHA_ERR_INVALID_ARG, "out_rows is null");
+    const int32_t rc = check_prompt(p, false);
+    if (rc) return rc;
+    *out_rows = plan_prompt(p).rows;
+    return AHA_OK;
+}
+
 int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, const void *v, const int32_t *first, void *out, float *lse,
                              void *workspace, size_t workspace_bytes, void *stream) {
     int32_t rc = check_prompt(p, true);
