@@ -552,7 +552,7 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
 typedef struct aha_prompt {
     int32_t tokens;       /* >= 1; tokens * n_q_heads <= 2^30 */
     int32_t sequences;    /* 1..65535 */
-    int32_t n_q_heads;    /* a multiple of n_kv_heads */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads, up to 2^25 times as many */
     int32_t n_kv_heads;   /* <= 65535 */
     int32_t head_dim;     /* 64 or 128 */
     int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, k, v and out */

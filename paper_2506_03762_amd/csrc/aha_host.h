@@ -296,6 +296,7 @@ struct PromptGeom {
     float *lse;
     const int32_t *first;
     int64_t qs[2], ks[2], vs[2], os[2];  // element strides: token, head
+    int item0;  // of a launch's first workgroup
     int tokens, sequences, Hq, Hkv, G, d, dtype;
     float c_out;  // scale times log2(e), above 0
 };

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
     __shared__ __attribute__((aligned(1024))) char smem[STAGED ? narrow_lds<T, D, true>() : A::lds];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane % ROWS;
     PromptTile it;
-    if (!prompt_tile(g, ROWS, (int)blockIdx.x, lane, it)) return;
+    if (!prompt_tile(g, ROWS, g.item0 + (int)blockIdx.x, lane, it)) return;
     KeyPlaces<T> keys;
     keys.in_a_row((const T *)g.k + it.lo * g.ks[0] + it.h * g.ks[1], (const T *)g.v + it.lo * g.vs[0] + it.h * g.vs[1], g.ks[0], g.vs[0]);
     keys.begin = 0;
@@ -65,8 +65,7 @@ __global__ __launch_bounds__(256, (kNarrowWorkgroups<T, D>)) void prompt_narrow_
 
 template <class T, int D, int ROWS, bool STAGED>
 static hipError_t launch_narrow(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {
-    hipLaunchKernelGGL((prompt_narrow_kernel<T, D, ROWS, STAGED>), dim3((unsigned)pl.items), dim3(256), 0, st, g);
-    return hipGetLastError();
+    return launch_prompt_items(prompt_narrow_kernel<T, D, ROWS, STAGED>, g, pl, 0, st);
 }
 
 hipError_t launch_prompt_attention(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {

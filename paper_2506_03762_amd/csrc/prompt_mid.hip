@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256, 2) void prompt_mid_kernel(PromptGeom g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     PromptUnits it;
-    if (!prompt_units<32>(g, (int)blockIdx.x, lane, it)) return;
+    if (!prompt_units<32>(g, g.item0 + (int)blockIdx.x, lane, it)) return;
     const int unit = it.first + wave, hq = it.h * g.G + unit % g.G, row0 = unit / g.G * 32;  // the wave's rows, counted from the prompt's start
     const int rows_here = max(0, min(32, it.n - row0));
     const __bf16 *kbase = (const __bf16 *)g.k + it.lo * g.ks[0] + it.h * g.ks[1], *vbase = (const __bf16 *)g.v + it.lo * g.vs[0] + it.h * g.vs[1];
@@ -216,8 +216,7 @@ static hipError_t launch_mid_t(const PromptGeom &g, const PromptPlan &pl, hipStr
         return hipFuncSetAttribute((const void *)prompt_mid_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)PromptMid<D>::bytes);
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(prompt_mid_kernel<D>, dim3((unsigned)pl.items), dim3(256), PromptMid<D>::bytes, st, g);
-    return hipGetLastError();
+    return launch_prompt_items(prompt_mid_kernel<D>, g, pl, PromptMid<D>::bytes, st);
 }
 
 hipError_t launch_prompt_mid(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {

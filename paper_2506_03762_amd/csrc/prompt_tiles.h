@@ -1,9 +1,25 @@
 // Which rows a workgroup of the attention of packed prompts takes.
 #pragma once
 
+#include <algorithm>
+
 #include "key_places.h"
 
 namespace aha {
+
+// The items of `pl`: a launch has fewer than 2^32 threads, so more than 2^23 workgroups of 256 take several (rows of a grid, whose width every workgroup has
+// to read, cost all calls 0.2 us).
+template <class Kernel>
+static hipError_t launch_prompt_items(Kernel kernel, PromptGeom g, const PromptPlan &pl, size_t lds, hipStream_t st) {
+    constexpr int64_t kMost = 1 << 23;
+    for (int64_t i = 0; i < pl.items; i += kMost) {
+        g.item0 = (int)i;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(kMost, pl.items - i)), dim3(256), lds, st, g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 // prompt s: [lo, lo + n)
 __device__ __forceinline__ int prompt_of(const PromptGeom &g, int s, int &lo) {

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256, 1) void prompt_wide_kernel(PromptGeom g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, hf = lane >> 5;
     PromptUnits it;
-    if (!prompt_units<64>(g, (int)blockIdx.x, lane, it)) return;
+    if (!prompt_units<64>(g, g.item0 + (int)blockIdx.x, lane, it)) return;
     const int unit = it.first + wave, hq = it.h * g.G + unit % g.G, row0 = unit / g.G * 64;  // the wave's rows, counted from the prompt's start
     const int rows_here = max(0, min(64, it.n - row0));
     KeyPlaces<__bf16> keys;
@@ -103,8 +103,7 @@ static hipError_t launch_wide_t(const PromptGeom &g, const PromptPlan &pl, hipSt
         return hipFuncSetAttribute((const void *)prompt_wide_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)PromptWide<D>::bytes);
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(prompt_wide_kernel<D>, dim3((unsigned)pl.items), dim3(256), PromptWide<D>::bytes, st, g);
-    return hipGetLastError();
+    return launch_prompt_items(prompt_wide_kernel<D>, g, pl, PromptWide<D>::bytes, st);
 }
 
 hipError_t launch_prompt_wide(const PromptGeom &g, const PromptPlan &pl, hipStream_t st) {

@@ -200,8 +200,9 @@ static int32_t check_prompt(const aha_prompt *p, bool strides) {
     if (rc) return rc;
     if (p->n_q_heads % p->n_kv_heads != 0)
         return fail(AHA_ERR_INVALID_ARG, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
-    if (p->sequences > 65535 || p->n_kv_heads > 65535 || (int64_t)p->tokens * p->n_q_heads > 1 << 30)
-        return fail(AHA_ERR_UNSUPPORTED, "sequences or n_kv_heads exceeds 65535 or tokens * n_q_heads 2^30");
+    // (a tile has a row at least, and the numbers of the tiles of 16 and 32 rows are rounded up to a group of eight: fewer than 2^31)
+    if (p->sequences > 65535 || p->n_kv_heads > 65535 || (int64_t)p->tokens * p->n_q_heads > 1 << 30 || p->n_q_heads / p->n_kv_heads > 1 << 25)
+        return fail(AHA_ERR_UNSUPPORTED, "sequences or n_kv_heads exceeds 65535, tokens * n_q_heads 2^30 or n_q_heads / n_kv_heads 2^25");
     if ((rc = check_scale("scale", p->scale))) return rc;
     if (p->reserved != 0) return fail(AHA_ERR_INVALID_ARG, "reserved must be 0");
     if (!strides) return AHA_OK;
@@ -236,6 +237,7 @@ static PromptPlan plan_prompt(const aha_prompt *p) {
                                                     {{16, 16, 256, 5.41f, 1.18f, .67f}, {32, 32, 256, 9.29f, 1.15f, .73f}}};  // d = 128
     float least = INFINITY;
     auto try_tiles = [&](const PromptTiles &t) {
+        if (p->tokens / t.rows > 1 << 25) return;  // (tile_of() counts fewer than 2^26 tiles to a prompt: 16 rows, 2^29 tokens)
         const int64_t units = (n + t.unit - 1) / t.unit * group, heads = t.rows / t.unit;  // (a tile of 32 rows: one unit)
         const int64_t tiles = prompts * ((units + heads - 1) / heads) * p->n_kv_heads;
         const float keys = t.block * (float)n / 32;
@@ -471,8 +473,6 @@ int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, 
         (rc = check_ptr("first", first, 4)) || (lse && (rc = check_ptr("lse", lse, 4))))
         return rc;
     const PromptPlan pl = plan_prompt(p);
-    // (workgroups of 256 threads: a launch has fewer than 2^32)
-    if (pl.items > 1 << 23) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
     if ((rc = check_ws(workspace, workspace_bytes, 0))) return rc;
     PromptGeom g{};
     g.q = q; g.k = k; g.v = v; g.out = out; g.lse = lse; g.first = first;
