@@ -583,7 +583,7 @@ int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, 
  */
 typedef struct aha_paged {
     int32_t batch;        /* batch * n_kv_heads <= 65535, batch * n_q_heads <= 2^22 */
-    int32_t n_q_heads;    /* a multiple of n_kv_heads; not looked at by aha_paged_evict */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads, up to 1024 times as many; not looked at by aha_paged_evict */
     int32_t n_kv_heads;
     int32_t head_dim;     /* 64 or 128 */
     int32_t dtype;        /* AHA_F32 | AHA_BF16: of q, pools and out */

@@ -309,6 +309,8 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     // (no part of more than 1024 places: sequences' lengths differ.  64 of up to 4096 tokens, 8 heads: 168 us with one part each, 160 with four, 167 with
     // eight)
     pl.parts = (int)std::max(parts_for(units * pl.tiles, room, 32), std::min<int64_t>(64, room / 1024));
+    // (workgroups of 256 threads: a launch has fewer than 2^32.  At most 2^22 rows in 65535 (sequence, KV head) pairs: 43 parts at least)
+    pl.parts = (int)std::min<int64_t>(pl.parts, (1 << 23) / (units * pl.tiles));
     // One launch where parts would shorten the chain of a sequence's blocks by less than the second one takes.  us with parts and in one, d = 128 (64), 64
     // (sequence, KV head) pairs, 4 query heads each: 256 tokens 12.0, 10.5 (10.9, 8.9), 384 12.2, 13.0 (11.1, 9.9), 768 15.3, 17.9 (13.2, 13.2); 128 pairs: 512
     // 16.3, 15.1 (13.6, 11.6), 768 20.9, 19.0 (15.7, 13.7), 1000 22.8, 23.0 (16.3, 16.0); 512 pairs of 400, which are never split, 29.9, 24.0; fp32, whose
@@ -328,10 +330,6 @@ static PagedPlan plan_paged(const aha_paged *p, const aha_pages *pages) {
     }
     pl.bytes = align_up(pl.off_dots + sizeof(float) * rows * (size_t)pl.ld, 256);
     return pl;
-}
-static int32_t check_paged_items(const PagedPlan &pl) {
-    if (pl.items > 1 << 23) return fail(AHA_ERR_UNSUPPORTED, "problem exceeds the launch grid limits");
-    return AHA_OK;
 }
 
 static int32_t check_evict(const aha_paged *p, const aha_pages *pg, bool strides) {
@@ -486,11 +484,9 @@ int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, 
 
 int32_t aha_paged_attention_workspace_bytes(const aha_paged *p, const aha_pages *pages, size_t *out_bytes) {
     if (!out_bytes) return fail(AHA_ERR_INVALID_ARG, "out_bytes is null");
-    int32_t rc = check_paged_attention(p, pages, false);
+    const int32_t rc = check_paged_attention(p, pages, false);
     if (rc) return rc;
-    const PagedPlan pl = plan_paged(p, pages);
-    if ((rc = check_paged_items(pl))) return rc;
-    *out_bytes = pl.bytes;
+    *out_bytes = plan_paged(p, pages).bytes;
     return AHA_OK;
 }
 
@@ -508,7 +504,7 @@ int32_t aha_paged_attention(const aha_paged *p, const aha_pages *pages, const vo
                          (pos && ((rc = check_ptr("pos", pos, 4)) || (rc = check_slots("pos", p->pos_stride, p, true))))))
         return rc;
     const PagedPlan pl = plan_paged(p, pages);
-    if ((rc = check_paged_items(pl)) || (rc = check_ws(workspace, workspace_bytes, pl.bytes))) return rc;
+    if ((rc = check_ws(workspace, workspace_bytes, pl.bytes))) return rc;
     PagedGeom g{};
     g.q = q; g.kt = k_pages; g.vt = v_pages; g.out = out; g.lse = lse; g.scores = scores; g.pos = pos; g.seen = seen;
     for (int t = 0; t < 2; ++t) {
