@@ -544,7 +544,8 @@ int32_t aha_shared_attention(const aha_shared *p, const aha_pages *pages, const 
  *              theirs is looked at, their rows of out and lse stay as they are.
  *  lse         out, fp32 dense [n_q_heads, tokens] or NULL: natural logarithm of
  *              sum_j exp(scale * q . K_j).  The last `window` columns of a prompt are what
- *              aha_prefill_scores_lse takes for it (scale_mode FIXED, the same scale).
+ *              aha_prefill_scores_lse takes for it, a prompt to a call, copied to a dense array
+ *              (scale_mode FIXED, the same scale).
  * The products' sums and the softmax are fp32; with AHA_BF16 the weights are rounded to bf16 where they
  * meet the values.  The VALUES of a prompt have to be finite (an infinite one reaches rows before it);
  * keys may be anything, a row knows those that it sees.
@@ -574,7 +575,9 @@ int32_t aha_prompt_attention(const aha_prompt *p, const void *q, const void *k, 
 
 /*
  * Single tokens over paged caches with running scores, and eviction from them (the generation of
- * Alg. 1 on a batch of caches of different lengths).
+ * Alg. 1 on a batch of caches of different lengths).  Two switches of aha_params are not built for them:
+ * decode_value_prior (weights are added to the running scores as they are) and score_pool (tokens go by
+ * their own scores).
  *
  * Token j of sequence b has, for KV head h, its key and value in the pages, its running score in
  * scores[b, h, j] and its position in pos[b, h, j].  A sequence has tail_len[b] tokens (as

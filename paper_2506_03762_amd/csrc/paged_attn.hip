@@ -2,8 +2,8 @@
 //
 //   out = sum_j softmax_j(scale q . K_j) V_j        F_j += sum_g softmax_j(lambda q_g . K_j)
 //
-// in two launches.  The first takes the keys of a (sequence, KV head) in parts: the rows of its query heads, padded to a tile of 32, in one pass
-// over the part's keys and values (narrow_tile.h), which leaves the products, a partial output and the sums of both softmaxes, relative
+// in two launches.  The first takes the keys of a (sequence, KV head) in parts: the rows of its query heads, padded to tiles of 32 (narrow_tile.h; fp32 with up to 16
+// heads one of 16, small_tile.h), in one pass over the part's keys and values, which leaves the products, a partial output and the sums of both softmaxes, relative
 // to references of their own, in the workspace.  The second joins the parts: outputs by row, scores by range of keys.  Where there is one part, its
 // workgroup does that itself (plan_paged() says when).
 //

@@ -3,9 +3,14 @@
 // A wave takes 32 rows of a query head; the four waves, heads of a group first, see nearly the same keys, whose rows and values' rows come to LDS once for
 // all of them, 32 keys to a stage, straight from global memory.  Two workgroups share a CU, so that one multiplies while the other one starts, waits or
 // writes its outputs, for which a tile of 256 rows (prompt_wide.hip) holds a CU for 10 us: 16 prompts of 200 tokens, 32 heads of 128 over 8, 24.5 us instead
-// of 32, of 500 69 instead of 78, one of 1024 27 instead of 35.  A wave reads every key and value from LDS for 32 rows only, twice as much per product,
-// which bounds it beyond that: one prompt of 16384 2085 us instead of 1890 (matrix cores 49 % busy; a third workgroup per CU, with three stages and no
-// products ahead, 2331; stages of 64 keys 2223; keys and values in registers a phase ahead, as in wide_tile.h, 2081).
+// of 32, of 500 69 instead of 78, one of 1024 27 instead of 35.
+//
+// Bound by a tile's start and end, as far as the second workgroup does not hide them: 18432 tokens in equal prompts of 288 to 1536, 32 heads of 128 over 8, take
+// 0.88 us per round of 512 tiles and block of 32 keys, which is what the matrix cores need (1.2 PFLOP/s), and 9.1 us per round besides (d = 64 0.57 and 3.7).
+// So 24 prompts of up to 1500 tokens, 11.4 rounds, 257 us, spend 100 of them there (matrix cores 36 % busy, LDS instructions issue in 4 % of the
+// waves' cycles).  Long prompts go to tiles of 256 rows, which read half as much from LDS per product: one of 16384 1935 us, here 2085 (matrix cores
+// 49 % busy, so LDS at half of its rate; a third workgroup per CU, with three stages and no products ahead, 2331; stages of 64 keys 2223; keys and
+// values in registers a phase ahead, as in wide_tile.h, 2081).
 #include <type_traits>
 
 #include "narrow_tile.h"
